@@ -448,6 +448,82 @@ int bz_op_gemm_plan(int mode, int M, int N, int K, size_t workspace_bytes, bz_ge
 int bz_op_gemm_static(int mode, const void* a, const void* w, const void* r, void* c, int M, int N, int K,
                       void* stream);
 
+/* ---- paged KV cache ---------------------------------------------------------------------------- */
+/* A cache in pages, for engines that run a layer by single operations: memory is dealt out page by page instead of in one
+ * run of positions per slot, rows may share the pages of a common prefix, and pages that have left a sliding window can be
+ * given back.  The batch says which rows of the table its sequences are (seq_slot) and how long they are; it is the same
+ * object that bz_run_layers takes.
+ *
+ * A page holds page_size positions of every kv head; k and v are [n_pages][n_kv_heads][page_size * head_dim] elements.  The
+ * page_size * head_dim elements of a (page, head) are blocks of 32 positions in the order in which the matrix instructions
+ * read them.  With position p = 16 t + 8 a + 4 h + b of a block (t, a, h < 2, b < 4) and head dim j < d:
+ *   BZ_KV_ACT:  key at ((j/8) * 32 + p) * 8 + j%8,     value at ((2 t + h) * d + j) * 8 + 4 a + b   (as in a slot's cache);
+ *   BZ_KV_E4M3: key at ((j/16) * 32 + p) * 16 + j%16,  value at (h * d + j) * 16 + 8 t + 4 a + b.
+ * BZ_KV_E4M3 holds OCP e4m3 numbers: a stored x stands for x * k_scale (x * v_scale).
+ * Memory need not be cleared: what lies at positions that no query sees, NaN included, has no effect on results.
+ *
+ * page_table[row * pages_per_row + i] is the page of positions page_size * i .. of that row.  Rows may name the same page;
+ * two sequences of one batch must not append to the same position of it.  An entry outside [0, n_pages) (-1) is a page that
+ * is not there: nothing is appended to its positions, no query sees them, and they read as zero.  Operations read the table,
+ * like the batch's lengths, when they run on the device. */
+enum { BZ_KV_ACT = 0, BZ_KV_E4M3 = 1 };
+typedef struct bz_paged_kv {
+    void*          k;               /* device, bz_paged_kv_bytes() bytes, 16-byte aligned */
+    void*          v;               /* the same */
+    const int32_t* page_table;      /* device, [n_rows][pages_per_row] */
+    int32_t        n_pages;
+    int32_t        page_size;       /* a power of two from 32 to 1024 */
+    int32_t        n_rows;
+    int32_t        pages_per_row;   /* pages_per_row * page_size < 2^31 */
+    int32_t        n_kv_heads;
+    int32_t        head_dim;        /* 64 or 128 */
+    int32_t        dtype;           /* BZ_KV_ACT: activation elements; BZ_KV_E4M3: bytes */
+    float          k_scale;         /* BZ_KV_E4M3: positive and finite; BZ_KV_ACT: 1 */
+    float          v_scale;
+} bz_paged_kv;
+
+/* Bytes of k, and of v; 0 if a field is out of range (pointers are not looked at). */
+size_t bz_paged_kv_bytes(const bz_paged_kv* kv);
+/* Cosines and sines for the operations below: out (host) is [positions][head_dim/2][2] floats, pair j of position p turned by
+ * p * base^(-2j/head_dim), angles in float64.  head_dim even, base > 1. */
+int bz_rope_table(int positions, int head_dim, float base, float* out);
+
+/* Appends the batch's new tokens: token i of sequence s goes to position kv_len_before[s] + i of row seq_slot[s].  k and v hold
+ * n_kv_heads * head_dim activation elements per packed row, rows k_stride and v_stride elements apart (multiples of 8; pointers
+ * 16-byte aligned), as they lie in the output of the QKV projection.  With `rope` (device, a table of rope_positions positions
+ * as bz_rope_table writes it) keys are rotated on the way, element j with j + head_dim/2; NULL: they are stored as they are.
+ * A rotated key and a value are rounded once, to the cache's type; in BZ_KV_E4M3 finite values and infinities beyond the largest
+ * e4m3 number (448) are stored as that, NaN as NaN.  Positions that the batch does not append keep their contents.
+ * BZ_EINVAL for a bad argument, BZ_ECAPACITY if a sequence outgrows its row of the table or the rotary table. */
+int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const float* rope, int rope_positions, void* stream);
+
+/* Attention of the batch's new tokens over the pages, which hold them already (bz_op_paged_append comes first): query head h of
+ * the token at position p reads kv head h / (n_q_heads / n_kv_heads) at positions 0..p, with window > 0 only at the last `window`
+ * of them, p itself included.  Scores are multiplied by `scale` (positive and finite; 0: 1/sqrt(head_dim)).  q and out hold
+ * n_q_heads * head_dim activation elements per packed row, rows q_stride and out_stride elements apart (multiples of 8; pointers
+ * 16-byte aligned); they may be the same memory only if strides agree as well.  `rope`: as above, queries are rotated as they are
+ * read; NULL: they are rotated already, or there is no rotation.  A query that sees no position gets zeros.  Sequences without new tokens and rows of out
+ * behind the last sequence are left alone.  Softmax and sums are float; weights are rounded to bf16 for the product with the values.
+ * A value that is not finite shows in every query that sees it, and may show in queries of the same sequence and call that come
+ * before it.  `workspace`: device scratch, 16-byte aligned, of at least bz_op_paged_attention_workspace_bytes() bytes for the same
+ * batch, shapes and window (BZ_ENOMEM if smaller); calls that may overlap in time need workspaces of their own.
+ * Results depend within rounding on the other sequences of the batch, whose lengths say how key ranges are cut; the same call
+ * gives the same bits every time.
+ *
+ * Both operations may be captured into a graph.  It replays the batch as it was: rebuilding, advancing or destroying the batch
+ * means capturing again, and is not ordered behind replays by the library.  Under capture a batch that was last rebuilt or
+ * advanced on another stream is refused (BZ_ESTATE). */
+size_t bz_op_paged_attention_workspace_bytes(const bz_batch* batch, const bz_paged_kv* kv, int n_q_heads, int window);
+int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const void* q, int64_t q_stride, void* out,
+                          int64_t out_stride, int n_q_heads, float scale, int window, const float* rope, int rope_positions,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Reads n >= 0 positions from pos0 on of table row `row`: k and v (device, 16-byte aligned) are [n, n_kv_heads, head_dim] activation
+ * elements, the layout that bz_kv_write takes: how a sequence leaves the pages for another instance.  BZ_ECAPACITY if the
+ * positions run past the row. */
+int bz_op_paged_read(const bz_paged_kv* kv, int row, int pos0, int n, void* k, void* v, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,6 +13,7 @@ from .binding import (  # noqa: F401
     BzError,
     Instance,
     KERNEL_CLASSES,
+    PagedKv,
     SIGNATURES,
     TENSOR_ORDER,
     load_library,
@@ -21,6 +22,11 @@ from .binding import (  # noqa: F401
     op_gemm_plan,
     op_gemm_static,
     op_gemm_workspace_bytes,
+    op_paged_append,
+    op_paged_attention,
+    op_paged_attention_workspace_bytes,
+    op_paged_read,
     op_rmsnorm,
     plan_generate,
+    rope_table,
 )

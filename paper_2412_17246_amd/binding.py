@@ -106,6 +106,14 @@ class bz_gemm_plan(C.Structure):
                 ("tiles_n", C.c_int), ("whole_tiles", C.c_int), ("ranges", C.c_int), ("workspace_bytes", C.c_size_t)]
 
 
+class bz_paged_kv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_rows", C.c_int32), ("pages_per_row", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_float), ("v_scale", C.c_float)]
+
+
+BZ_KV_ACT, BZ_KV_E4M3 = 0, 1
+
 BZ_GEMM_SMALL, BZ_GEMM_DECODE, BZ_GEMM_MID, BZ_GEMM_LARGE = 0, 1, 2, 3
 
 # name -> (restype, argtypes); also the list of symbols the header declares
@@ -170,6 +178,13 @@ SIGNATURES = {
     "bz_op_gemm": (C.c_int, [C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_int, _P, C.c_size_t, _P]),
     "bz_op_gemm_plan": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_size_t, C.POINTER(bz_gemm_plan)]),
     "bz_op_gemm_static": (C.c_int, [C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_int, _P]),
+    "bz_paged_kv_bytes": (C.c_size_t, [C.POINTER(bz_paged_kv)]),
+    "bz_rope_table": (C.c_int, [C.c_int, C.c_int, C.c_float, _P]),
+    "bz_op_paged_append": (C.c_int, [_P, C.POINTER(bz_paged_kv), _P, C.c_int64, _P, C.c_int64, _P, C.c_int, _P]),
+    "bz_op_paged_attention_workspace_bytes": (C.c_size_t, [_P, C.POINTER(bz_paged_kv), C.c_int, C.c_int]),
+    "bz_op_paged_attention": (C.c_int, [_P, C.POINTER(bz_paged_kv), _P, C.c_int64, _P, C.c_int64, C.c_int, C.c_float,
+                                        C.c_int, _P, C.c_int, _P, C.c_size_t, _P]),
+    "bz_op_paged_read": (C.c_int, [C.POINTER(bz_paged_kv), C.c_int, C.c_int, C.c_int, _P, _P, _P]),
 }
 
 _libs: Dict[str, C.CDLL] = {}
@@ -630,3 +645,107 @@ def op_gemm_static(mode: int, a, w, r, c, M: int, N: int, K: int, stream=None, f
     rc = lib.bz_op_gemm_static(mode, _ptr(a), _ptr(w), _ptr(r), _ptr(c), M, N, K, stream.cuda_stream if stream else 0)
     if rc:
         raise BzError(rc, "bz_op_gemm_static", lib.bz_last_hip_error().decode() if rc == -6 else "")
+
+
+def rope_table(positions: int, head_dim: int, base: float, fp32_debug: bool = False) -> np.ndarray:
+    """Cosines and sines [positions, head_dim/2, 2] (float32) for the `rope` argument of the paged operations."""
+    out = np.empty((max(positions, 0), max(head_dim, 0) // 2, 2), dtype=np.float32)
+    rc = load_library(fp32_debug).bz_rope_table(positions, head_dim, base, out.ctypes.data)
+    if rc:
+        raise BzError(rc, "bz_rope_table")
+    return out
+
+
+class PagedKv:
+    """A paged KV cache in memory of the caller's: `k` and `v` are contiguous tensors of n_pages * n_kv_heads * page_size *
+    head_dim elements, bf16 (float in the fp32 debug build) or float8_e4m3fn, `page_table` a contiguous int32 tensor
+    [rows, pages per row] on the same device; a batch's seq_slot says which row a sequence is."""
+
+    def __init__(self, page_size: int, n_kv_heads: int, head_dim: int, *, k, v, page_table, k_scale: float = 1.0,
+                 v_scale: float = 1.0, fp32_debug: bool = False):
+        import torch
+        act = torch.float32 if fp32_debug else torch.bfloat16
+        if k.dtype not in (act, torch.float8_e4m3fn) or v.dtype != k.dtype or page_table.dtype != torch.int32:
+            raise ValueError(f"k and v must be {act} or float8_e4m3fn, both the same, and page_table int32")
+        if page_table.dim() != 2 or not (k.is_contiguous() and v.is_contiguous() and page_table.is_contiguous()):
+            raise ValueError("k, v and the two-dimensional page_table must be contiguous")
+        if not (k.is_cuda and k.device == v.device == page_table.device):
+            raise ValueError("k, v and page_table must be on one GPU")
+        page = page_size * n_kv_heads * head_dim
+        if page < 1 or k.numel() % page or k.numel() != v.numel():
+            raise ValueError("k and v must hold the same number of whole pages")
+        self.k, self.v, self.page_table, self.fp32_debug = k, v, page_table, fp32_debug
+        self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
+        self.desc = bz_paged_kv(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), k.numel() // page, page_size,
+                                page_table.shape[0], page_table.shape[1], n_kv_heads, head_dim,
+                                BZ_KV_E4M3 if k.dtype == torch.float8_e4m3fn else BZ_KV_ACT, k_scale, v_scale)
+        self.lib = load_library(fp32_debug)
+        if self.lib.bz_paged_kv_bytes(C.byref(self.desc)) != k.numel() * k.element_size():
+            raise BzError(-1, "bz_paged_kv")
+        self._ref = C.byref(self.desc)
+        self._act = act
+
+
+def _rows(kv: PagedKv, batch: Batch, x, what: str) -> int:
+    """Checks the packed rows of a batch's heads and returns how many elements a row has."""
+    if x.dim() != 2 or x.shape[0] < batch.T or x.stride(1) != 1 or x.dtype != kv._act or x.device != kv.k.device:
+        raise ValueError(f"{what} must be [{batch.T} rows or more, heads * head_dim] of {kv._act} on {kv.k.device}, "
+                         "the elements of a row side by side")
+    return x.shape[1]
+
+
+def _pitch(x) -> int:
+    """Elements from a row to the next (torch may say anything where there is only one)."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _rope(kv: PagedKv, rope):
+    if rope is None:
+        return 0, 0
+    if rope.shape[1:] != (kv.head_dim // 2, 2) or not rope.is_contiguous() or rope.element_size() != 4 or rope.device != kv.k.device:
+        raise ValueError("rope must be a contiguous float32 tensor [positions, head_dim/2, 2] on the cache's device")
+    return rope.data_ptr(), rope.shape[0]
+
+
+def op_paged_append(batch: Batch, kv: PagedKv, k, v, rope=None, stream=None) -> None:
+    """Appends the batch's keys (rotated on the way with `rope`) and values, [T, n_kv_heads * head_dim] each, to the pages;
+    both may be columns of one wider tensor."""
+    width = kv.n_kv_heads * kv.head_dim
+    if _rows(kv, batch, k, "k") != width or _rows(kv, batch, v, "v") != width:
+        raise ValueError("a row of k and v must be n_kv_heads * head_dim elements")
+    tab, positions = _rope(kv, rope)
+    rc = kv.lib.bz_op_paged_append(batch.handle, kv._ref, k.data_ptr(), _pitch(k), v.data_ptr(), _pitch(v), tab,
+                                   positions, stream.cuda_stream if stream else 0)
+    if rc:
+        raise BzError(rc, "bz_op_paged_append", kv.lib.bz_last_hip_error().decode() if rc == -6 else "")
+
+
+def op_paged_attention_workspace_bytes(batch: Batch, kv: PagedKv, n_q_heads: int, window: int = 0) -> int:
+    return int(kv.lib.bz_op_paged_attention_workspace_bytes(batch.handle, kv._ref, n_q_heads, window))
+
+
+def op_paged_attention(batch: Batch, kv: PagedKv, q, out, scale: float = 0.0, window: int = 0, rope=None, workspace=None,
+                       stream=None) -> None:
+    """Attention of the batch's new tokens, which the pages hold already, for q [T, n_q_heads * head_dim] into `out`."""
+    width = _rows(kv, batch, q, "q")
+    if _rows(kv, batch, out, "out") != width or width % kv.head_dim:
+        raise ValueError("a row of q and out must be n_q_heads * head_dim elements")
+    tab, positions = _rope(kv, rope)
+    rc = kv.lib.bz_op_paged_attention(batch.handle, kv._ref, q.data_ptr(), _pitch(q), out.data_ptr(), _pitch(out),
+                                      width // kv.head_dim, scale, window, tab, positions,
+                                      workspace.data_ptr() if workspace is not None else 0,
+                                      workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                      stream.cuda_stream if stream else 0)
+    if rc:
+        raise BzError(rc, "bz_op_paged_attention", kv.lib.bz_last_hip_error().decode() if rc == -6 else "")
+
+
+def op_paged_read(kv: PagedKv, row: int, pos0: int, n: int, k, v, stream=None) -> None:
+    """Positions pos0 .. pos0 + n - 1 of a table row into k and v, contiguous [n, n_kv_heads, head_dim]."""
+    need = n * kv.n_kv_heads * kv.head_dim
+    for x in (k, v):
+        if x.dtype != kv._act or x.device != kv.k.device or not x.is_contiguous() or x.numel() < need:
+            raise ValueError(f"k and v must be contiguous {kv._act} tensors of [n, n_kv_heads, head_dim] on the cache's device")
+    rc = kv.lib.bz_op_paged_read(kv._ref, row, pos0, n, k.data_ptr(), v.data_ptr(), stream.cuda_stream if stream else 0)
+    if rc:
+        raise BzError(rc, "bz_op_paged_read", kv.lib.bz_last_hip_error().decode() if rc == -6 else "")

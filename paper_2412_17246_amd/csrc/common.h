@@ -206,6 +206,7 @@ struct BatchView {
     int prefill_keys;              // longest key range of a prefill item
     const int32_t* decode_seqs;    // [n_decode] sequence indices with exactly one new token
     int n_decode;
+    const int32_t* short_seqs;     // sequence indices with 2 to kShortTokens new tokens, fewest first
     int decode_chunks;             // upper bound on ceil((kv_before+1)/kDecodeChunk) over decode seqs
     // One entry (two int4) per (decode sequence, chunk of its cache) that exists now, sequence by
     // sequence: (sequence index, KV slot, index into decode_seqs, chunks of this sequence), (index of
@@ -227,6 +228,7 @@ struct QkvSource {
 };
 
 constexpr int kPrefillTileQ = 128;   // query rows per prefill-attention workgroup
+constexpr int kShortTokens = 64;     // most new tokens of a sequence in BatchView::short_seqs
 constexpr int kDecodeChunk = 256;    // KV positions per decode-attention workgroup
 
 // ---- launchers (each enqueues on `st`; shapes are validated by the callers) ------------------

@@ -40,6 +40,7 @@ struct bz_batch {
     std::vector<int32_t> q_start, seq_slot, kv_before;
     int n_prefill_items = 0, prefill_keys = 0, n_decode = 0;
     std::vector<int32_t> decode_seqs;
+    std::vector<int32_t> short_seqs, short_qlen;   // sequences with 2 to kShortTokens new tokens, fewest first
     double prefill_sq = 0;            // sum over prefill sequences of visible (query, key) pairs
     void* dev = nullptr;              // one allocation holding all device arrays
     int32_t *d_q_start = nullptr, *d_seq_slot = nullptr, *d_kv_before = nullptr, *d_token_seq = nullptr,
@@ -66,6 +67,14 @@ struct bz_batch {
     hipEvent_t changed_ev = nullptr;
     bool changed_valid = false;
 };
+
+namespace bz {
+BatchView batch_view(const bz_batch* b);
+// around the kernels that read a batch on stream `st`
+int batch_before_run(const bz_batch* b, hipStream_t st);
+int batch_after_run(const bz_batch* b, hipStream_t st);
+int stream_is_capturing(hipStream_t st, bool* out);
+}  // namespace bz
 
 struct bz_instance {
     bz_config cfg;

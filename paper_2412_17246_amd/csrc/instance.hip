@@ -134,30 +134,6 @@ KvView kv_view(bz_instance* I, int layer) {
     return v;
 }
 
-BatchView batch_view(const bz_batch* b) {
-    BatchView v;
-    v.B = b->B;
-    v.T = b->T;
-    v.q_start = b->d_q_start;
-    v.seq_slot = b->d_seq_slot;
-    v.kv_before = b->d_kv_before;
-    v.token_seq = b->d_token_seq;
-    v.prefill_items = b->d_items;
-    v.n_prefill_items = b->n_prefill_items;
-    v.prefill_keys = b->prefill_keys;
-    v.decode_seqs = b->d_decode;
-    v.n_decode = b->n_decode;
-    int mx = 0, work = 0;
-    for (int s : b->decode_seqs) {
-        mx = mx > b->kv_before[s] + 1 ? mx : b->kv_before[s] + 1;
-        work += (b->kv_before[s] + 1 + kDecodeChunk - 1) / kDecodeChunk;
-    }
-    v.decode_chunks = (mx + kDecodeChunk - 1) / kDecodeChunk;
-    v.decode_work = b->d_work;
-    v.n_decode_work = work;             // the device list was built for these same lengths
-    return v;
-}
-
 int poll_layer(bz_instance* I, int l) {
     if (I->state[l] == kLoading) {
         hipError_t e = hipEventQuery(I->ev[l]);
@@ -773,6 +749,8 @@ int describe_batch(const bz_batch_desc* d, bz_batch* b, std::vector<int32_t>& im
     b->seq_slot.assign(d->seq_slot, d->seq_slot + B);
     b->kv_before.assign(d->kv_len_before, d->kv_len_before + B);
     b->decode_seqs.clear();
+    b->short_seqs.clear();
+    b->short_qlen.clear();
     b->prefill_sq = 0;
     std::vector<int32_t> token_seq(T), items;
     b->all_decode = true;
@@ -783,6 +761,7 @@ int describe_batch(const bz_batch_desc* d, bz_batch* b, std::vector<int32_t>& im
         for (int t = b->q_start[s]; t < b->q_start[s + 1]; ++t) token_seq[t] = s;
         if (qlen == 1) b->decode_seqs.push_back(s);
         if (qlen != 1) b->all_decode = false;
+        if (qlen > 1 && qlen <= kShortTokens) b->short_seqs.push_back(s);
         if (qlen > 1) {
             const int tiles = (qlen + kPrefillTileQ - 1) / kPrefillTileQ;
             for (int qt = 0; qt < tiles; ++qt) {
@@ -798,6 +777,10 @@ int describe_batch(const bz_batch_desc* d, bz_batch* b, std::vector<int32_t>& im
     b->n_prefill_items = (int)its.size();
     b->prefill_keys = its.empty() ? 0 : (int)std::min<long long>(its.front().extent, INT32_MAX);
     b->n_decode = (int)b->decode_seqs.size();
+    // sequences with a few new tokens, fewest first: those with at most so many are the first of the list
+    auto tokens = [&](int s) { return b->q_start[s + 1] - b->q_start[s]; };
+    std::stable_sort(b->short_seqs.begin(), b->short_seqs.end(), [&](int x, int y) { return tokens(x) < tokens(y); });
+    for (int s : b->short_seqs) b->short_qlen.push_back(tokens(s));
 
     // decode work list: one entry per chunk of every decode sequence's cache (the new token included), with
     // room for kWorkGrowth more chunks per sequence as bz_batch_advance lengthens the caches.  The room is
@@ -812,9 +795,15 @@ int describe_batch(const bz_batch_desc* d, bz_batch* b, std::vector<int32_t>& im
             work.insert(work.end(), entry, entry + 8);
         }
     }
-    const size_t n_i32 = (size_t)(B + 1) + B + B + T + items.size() + b->decode_seqs.size();
-    *work_at = align32(n_i32 * 4);
     const size_t present = work.size() / 8;
+    size_t n_i32 = (size_t)(B + 1) + B + B + T + items.size() + b->decode_seqs.size();
+    // the one list that a reader can do without
+    if (max_bytes && align32((n_i32 + b->short_seqs.size()) * 4) + present * 32 + 64 > max_bytes) {
+        b->short_seqs.clear();
+        b->short_qlen.clear();
+    }
+    n_i32 += b->short_seqs.size();
+    *work_at = align32(n_i32 * 4);
     size_t capacity = present + (size_t)kWorkGrowth * b->n_decode;
     if (max_bytes) {
         if (*work_at + present * 32 + 64 > max_bytes) return BZ_ECAPACITY;
@@ -831,6 +820,7 @@ int describe_batch(const bz_batch_desc* d, bz_batch* b, std::vector<int32_t>& im
     b->off_words[3] = put(token_seq);
     b->off_words[4] = put(items);
     b->off_words[5] = put(b->decode_seqs);
+    put(b->short_seqs);                                // behind them; every sequence is in one of the two at most
     image.resize(*work_at / 4, 0);
     image.insert(image.end(), work.begin(), work.end());
     image.resize((*work_at + capacity * 32 + 64) / 4, 0);
@@ -865,6 +855,79 @@ int mark_changed(bz_batch* b, hipStream_t st) {
 }
 
 }  // namespace
+
+}  // extern "C"
+
+namespace bz {
+BatchView batch_view(const bz_batch* b) {
+    BatchView v;
+    v.B = b->B;
+    v.T = b->T;
+    v.q_start = b->d_q_start;
+    v.seq_slot = b->d_seq_slot;
+    v.kv_before = b->d_kv_before;
+    v.token_seq = b->d_token_seq;
+    v.prefill_items = b->d_items;
+    v.n_prefill_items = b->n_prefill_items;
+    v.prefill_keys = b->prefill_keys;
+    v.decode_seqs = b->d_decode;
+    v.n_decode = b->n_decode;
+    v.short_seqs = b->d_decode + b->n_decode;
+    int mx = 0, work = 0;
+    for (int s : b->decode_seqs) {
+        mx = mx > b->kv_before[s] + 1 ? mx : b->kv_before[s] + 1;
+        work += (b->kv_before[s] + 1 + kDecodeChunk - 1) / kDecodeChunk;
+    }
+    v.decode_chunks = (mx + kDecodeChunk - 1) / kDecodeChunk;
+    v.decode_work = b->d_work;
+    v.n_decode_work = work;             // the device list was built for these same lengths
+    return v;
+}
+
+// Orders stream `st` behind the batch's last change if that was enqueued on another stream.
+int batch_before_run(const bz_batch* b, hipStream_t st) {
+    if (!b->changed_valid || b->changed_on == st) return BZ_OK;
+    bool capturing = false;
+    const int rc = stream_is_capturing(st, &capturing);
+    if (rc) return rc;
+    if (capturing) return BZ_ESTATE;         // the wait would be for work outside the capture
+    HIP_TRY(hipStreamWaitEvent(st, b->changed_ev, 0));
+    return BZ_OK;
+}
+
+// A batch that can change on the device later (advance, rebuild), possibly on another stream, gets a marker behind the
+// kernels that read it: one event per stream that ever ran it, re-recorded.
+int batch_after_run(const bz_batch* b, hipStream_t st) {
+    if (!b->all_decode && !b->staging) return BZ_OK;
+    bool capturing = false;
+    const int rc = stream_is_capturing(st, &capturing);
+    if (rc) return rc;
+    if (capturing) return BZ_OK;             // replays are the caller's to order
+    bz_batch::Use* use = nullptr;
+    for (bz_batch::Use& u : b->runs)
+        if (u.st == st) use = &u;
+    if (!use) {
+        hipEvent_t ev = nullptr;
+        HIP_TRY(hipEventCreateWithFlags(&ev, hipEventDisableTiming));
+        b->runs.push_back(bz_batch::Use{st, ev});
+        use = &b->runs.back();
+    }
+    HIP_TRY(hipEventRecord(use->ev, st));
+    return BZ_OK;
+}
+
+int stream_is_capturing(hipStream_t st, bool* out) {
+    *out = false;
+    if (!st) return BZ_OK;                   // the null stream cannot be captured
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    HIP_TRY(hipStreamIsCapturing(st, &status));
+    *out = status != hipStreamCaptureStatusNone;
+    return BZ_OK;
+}
+
+}  // namespace bz
+
+extern "C" {
 
 int bz_batch_destroy(bz_batch* b) {
     if (!b) return BZ_EINVAL;
@@ -1025,7 +1088,10 @@ int bz_run_layers(bz_instance* I, int a, int b, const bz_batch* batch, void* hid
     const Shape& sh = I->sh;
     const int T = batch->T;
     // the batch's device arrays may have been uploaded, or advanced, on another instance's stream
-    if (batch->changed_valid && batch->changed_on != I->compute) HIP_TRY(hipStreamWaitEvent(I->compute, batch->changed_ev, 0));
+    {
+        const int rc = batch_before_run(batch, I->compute);
+        if (rc) return rc;
+    }
     const BatchView bv = batch_view(batch);
     act_t* x = static_cast<act_t*>(hidden);
     act_t* normed = reinterpret_cast<act_t*>(I->wsp + I->ws.normed);
@@ -1129,19 +1195,9 @@ int bz_run_layers(bz_instance* I, int a, int b, const bz_batch* batch, void* hid
         launch_reduce_residual_rmsnorm(x, gws, pending_down, nullptr, normed, T, sh.H, I->cfg.rms_eps, st);
         HIP_TRY(hipGetLastError());
     }
-    if (batch->all_decode || batch->staging) {
-        // this batch can change on the device later (advance, rebuild), possibly on another stream: leave a
-        // marker behind the kernels that read it (one event per stream that ever ran it, re-recorded)
-        bz_batch::Use* use = nullptr;
-        for (bz_batch::Use& u : batch->runs)
-            if (u.st == st) use = &u;
-        if (!use) {
-            hipEvent_t ev = nullptr;
-            HIP_TRY(hipEventCreateWithFlags(&ev, hipEventDisableTiming));
-            batch->runs.push_back(bz_batch::Use{st, ev});
-            use = &batch->runs.back();
-        }
-        HIP_TRY(hipEventRecord(use->ev, st));
+    {
+        const int rc = batch_after_run(batch, st);
+        if (rc) return rc;
     }
     I->stats.tokens_run += (uint64_t)T * (uint64_t)(b - a);
     I->stats.layer_launches += (uint64_t)(b - a);

@@ -1,0 +1,101 @@
+// The paged KV cache: device view, element order, launchers of its operations.
+#pragma once
+
+#include "common.h"
+
+namespace bz {
+
+constexpr float kE4m3Max = 448.f;
+
+// Device-side view of a paged cache of one layer.  The elements of a (page, kv head) are blocks of 32 positions, each in the
+// order in which a 32x32x16 MFMA reads its row operand: of activation elements as in KvView; of e4m3, sixteen elements to the
+// 16 bytes a lane loads, which are two k-steps of the product:
+//   K: [d/16][position][16], a lane half h reading piece 2i + h holds dims 32i + 16h + 0..15 of its position;
+//   V: [h][j][16], the positions {4h + 0..3, 8 + 4h + 0..3} and the same 16 further on, of head dim j.
+struct PagedView {
+    void* k;
+    void* v;
+    const int32_t* table;      // [rows][per_row]
+    int n_pages, per_row, page_shift;
+    int Hkv, d;
+    float k_scale, v_scale;    // what 1 in the cache stands for
+    float k_inv, v_inv;        // and what the append multiplies by
+};
+
+struct PagedRope {
+    const float* tab;          // [positions][d/2] pairs of cos, sin; null: no rotation
+    int positions;
+};
+
+// Offset inside a block of 32 positions.
+template <bool E4M3>
+__host__ __device__ inline int k_block_offset(int p, int j) {
+    return E4M3 ? ((j >> 4) * 32 + p) * 16 + (j & 15) : ((j >> 3) * 32 + p) * 8 + (j & 7);
+}
+template <bool E4M3>
+__host__ __device__ inline int v_block_offset(int p, int j, int d) {
+    const int t = p >> 4, a = (p >> 3) & 1, h = (p >> 2) & 1, b = p & 3;
+    return E4M3 ? (h * d + j) * 16 + 8 * t + 4 * a + b : ((2 * t + h) * d + j) * 8 + 4 * a + b;
+}
+
+// Page that holds `pos` of table row `row`; -1 if it is not there.  Whatever the table holds, the result is in range.
+__device__ __forceinline__ int page_of(const PagedView& kv, int row, int pos) {
+    const int i = pos >> kv.page_shift;
+    if (i >= kv.per_row) return -1;
+    const int id = kv.table[(size_t)row * kv.per_row + i];
+    return id >= 0 && id < kv.n_pages ? id : -1;
+}
+// First element of the block of 32 positions that holds `pos`, in page `id`, of kv head `head`.
+__device__ __forceinline__ size_t block_base(const PagedView& kv, int id, int head, int pos) {
+    const int in_page = pos & ((1 << kv.page_shift) - 1) & ~31;
+    return ((((size_t)id * kv.Hkv + head) << kv.page_shift) + in_page) * kv.d;
+}
+// A position's row of the rotary table.  The host has checked the lengths; the bound holds for a captured graph that is
+// replayed on longer ones.
+__device__ __forceinline__ const float* rope_row(const PagedRope& rope, int pos, int d) {
+    return rope.tab + (size_t)(pos < rope.positions ? pos : rope.positions - 1) * d;
+}
+
+// Saturates to the largest e4m3 number; NaN stays.
+__device__ __forceinline__ float e4m3_range(float x) {
+    const float c = fminf(fmaxf(x, -kE4m3Max), kE4m3Max);
+    return x != x ? x : c;
+}
+__device__ __forceinline__ uint8_t to_e4m3(float x) {
+    return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x), 0.f, 0, false) & 0xff);
+}
+__device__ __forceinline__ float from_e4m3(uint8_t b) { return __builtin_amdgcn_cvt_f32_fp8((int)b, 0); }
+
+// One element of a cache, as the number it holds (scale not applied).
+template <bool E4M3>
+__device__ __forceinline__ float cache_get(const void* base, size_t at) {
+    if (E4M3) return from_e4m3(static_cast<const uint8_t*>(base)[at]);
+    return to_f32(static_cast<const act_t*>(base)[at]);
+}
+template <bool E4M3>
+__device__ __forceinline__ void cache_put(void* base, size_t at, float x) {
+    if (E4M3) static_cast<uint8_t*>(base)[at] = to_e4m3(x);
+    else from_f32(static_cast<act_t*>(base)[at], x);
+}
+
+void launch_paged_append(const act_t* k, size_t k_stride, const act_t* v, size_t v_stride, const PagedRope& rope, bool e4m3,
+                         const BatchView& bv, const PagedView& kv, hipStream_t st);
+void launch_paged_read(bool e4m3, const PagedView& kv, int row, int pos0, int n, act_t* k, act_t* v, hipStream_t st);
+
+struct PagedQuery {
+    const act_t* q;
+    act_t* out;
+    size_t q_stride, out_stride;
+    PagedRope rope;
+    int Hq, window;
+    float scale_log2;          // score scale times log2 e, and times what 1 in the K cache stands for
+};
+// What the attention of a batch needs to know of its lengths, from the host's copy of them.
+struct PagedWork {
+    int dummy;
+};
+size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, int Hkv, int d);
+void launch_paged_attention(const PagedQuery& q, const PagedWork& w, bool e4m3, const BatchView& bv, const PagedView& kv,
+                            float* ws, hipStream_t st);
+
+}  // namespace bz
