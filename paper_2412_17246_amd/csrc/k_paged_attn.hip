@@ -1,0 +1,828 @@
+// Attention of a batch's new tokens over a paged KV cache.
+//
+// A kv head's query heads and a sequence's new tokens are rows of one problem: row r of (sequence, kv head) is token r / G and
+// query head kvh * G + r % G, G = Hq / Hkv, so every K and V that a workgroup reads serves all rows it holds.  Per row, with
+// scores s_j in base 2 (scale times log2 e), m = max s_j, l = sum 2^(s_j - m), o = sum 2^(s_j - m) V_j / l, taken over the keys
+// in pieces: (m, l, o) of two pieces join as m' = max, l' = l 2^(m - m') + ..., o' likewise.  A piece in which a row sees nothing
+// has m = -inf, l = 0.
+//
+// Masked positions get weight 0, and 0 times a NaN is a NaN: values at positions that none of the workgroup's rows may see
+// (behind the sequence, before the window, on a page that is not there) are cleared before the product.
+#include "paged.h"
+
+namespace bz {
+
+#ifndef BZ_FP32_DEBUG
+namespace {
+
+typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// weights below the normal range flush to zero: the largest of a row's is 1
+__device__ __forceinline__ float exp2_flush(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// reference of a running maximum that may not have seen a key yet
+__device__ __forceinline__ float finite_or_0(float m) { return m > -INFINITY ? m : 0.f; }
+
+template <class T>
+__device__ __forceinline__ T stream_load(const T* p) { return __builtin_nontemporal_load(p); }
+
+// eight e4m3 numbers to bf16, which holds each of them exactly
+__device__ __forceinline__ bf16x8 e4m3_to_bf16(uint32_t a, uint32_t b) {
+    const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+    const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+    return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+
+// 8 pairs (j0 + e, j0 + e + d/2) of a query, rotated if there is a table, rounded to bf16
+__device__ __forceinline__ void rotate8(const bf16* q, const float* cs, int half, bf16x8& lo8, bf16x8& hi8) {
+    lo8 = *reinterpret_cast<const bf16x8*>(q);
+    hi8 = *reinterpret_cast<const bf16x8*>(q + half);
+    if (!cs) return;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float4 v = *reinterpret_cast<const float4*>(cs + 2 * e);
+        const float l0 = (float)lo8[e], h0 = (float)hi8[e], l1 = (float)lo8[e + 1], h1 = (float)hi8[e + 1];
+        lo8[e] = (bf16)(l0 * v.x - h0 * v.y);
+        hi8[e] = (bf16)(h0 * v.x + l0 * v.y);
+        lo8[e + 1] = (bf16)(l1 * v.z - h1 * v.w);
+        hi8[e + 1] = (bf16)(h1 * v.z + l1 * v.w);
+    }
+}
+
+__device__ __forceinline__ int first_seen(int pos, int window) { return window && pos + 1 > window ? pos + 1 - window : 0; }
+
+// Place of a narrow sequence's tokens among the partial results: single tokens first, then `short_tokens` per sequence.
+__device__ __forceinline__ size_t partial_at(const PagedWork& w, int n_decode, int i, int token, int Hq, int head, int chunk, int D) {
+    const int t = i < n_decode ? i : n_decode + (i - n_decode) * w.short_tokens + token;
+    return (((size_t)t * Hq + head) * w.max_chunks + chunk) * (D + 2);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------------------------
+// Narrow: a workgroup reads one chunk of 256 positions of one kv head once, for up to RT rows.  Each of its four waves owns 64
+// positions, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose row
+// operand is the cache as it lies in memory; rows of the problem are the 32 columns.  The four results are merged through LDS in wave
+// order.  Bound by the cache's bytes.
+// ---------------------------------------------------------------------------------------------
+template <int D, bool E4M3, int RT, int WAVES>
+__global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(256) void paged_narrow_kernel(
+    PagedQuery a, PagedWork w, BatchView bv, PagedView kv, float* __restrict__ partial) {
+    constexpr int CH = kDecodeChunk, KS = D / 16, DB = D / 32, LD = D + 8;
+    constexpr int NF = E4M3 ? D / 32 : D / 16;               // 16-byte loads per lane and block, of K and again of V
+    __shared__ float wmx[4][RT], wsum[4][RT];
+    __shared__ float osh[4][RT][D];
+    __shared__ __attribute__((aligned(16))) bf16 qs[RT][LD];
+
+    const int Hkv = kv.Hkv, G = a.Hq / Hkv;
+    const int listed = w.list * Hkv * w.col_tiles;
+    int i, s, row, kvh, ct, chunk;
+    if ((int)blockIdx.x < listed) {
+        const int per = Hkv * w.col_tiles, e = blockIdx.x / per;
+        const int4 item = bv.decode_work[2 * e];
+        const int rest = blockIdx.x - per * bv.decode_work[2 * e + 1].x;
+        s = item.x;
+        row = item.y;
+        i = item.z;
+        chunk = rest % item.w;
+        const int hc = rest / item.w;
+        kvh = hc / w.col_tiles;
+        ct = hc - kvh * w.col_tiles;
+    } else {
+        int rest = blockIdx.x - listed;
+        chunk = rest % w.chunks;
+        rest /= w.chunks;
+        ct = rest % w.col_tiles;
+        rest /= w.col_tiles;
+        kvh = rest % Hkv;
+        i = w.first + rest / Hkv;
+        s = bv.decode_seqs[i];
+        row = bv.seq_slot[s];
+    }
+    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
+    const int hi = before + n, lo = first_seen(before, a.window);
+    const int c0 = (lo & ~63) + chunk * CH;
+    const int r0 = ct * kNarrowRows, R = n * G;
+    if (c0 >= hi || r0 >= R || chunk >= w.max_chunks || kvh >= Hkv) return;
+    const int rows = R - r0 < RT ? R - r0 : RT;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lq = lane & 31, lh = lane >> 5;
+    const int w0 = c0 + wave * 64;
+    const bool live = w0 < hi;                               // wave-uniform
+    int id[2];
+    bool there[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int pos = w0 + 32 * b;
+        id[b] = pos < hi ? page_of(kv, row, pos) : -1;
+        there[b] = id[b] >= 0;
+        if (!there[b]) id[b] = 0;                            // read in bounds, masked below
+    }
+
+    // queries: unit = 8 pairs of a row, requested before the stream
+    constexpr int UPR = D / 16;
+    const int units = rows * UPR;
+    const int u = tid < units ? tid : units - 1;
+    const int ur = u / UPR, uj = (u - ur * UPR) * 8;
+    const int ut = (r0 + ur) / G, uh = kvh * G + (r0 + ur) - ut * G;
+    const bf16* qp = a.q + (size_t)(q0 + ut) * a.q_stride + uh * D + uj;
+    bf16x8 qlo = *reinterpret_cast<const bf16x8*>(qp), qhi = *reinterpret_cast<const bf16x8*>(qp + D / 2);
+    f32x4 cs[4] = {};
+    if (a.rope.tab) {
+        const float* c = rope_row(a.rope, before + ut, D) + 2 * uj;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs[e] = *reinterpret_cast<const f32x4*>(c + 4 * e);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    u32x4 kf[2][NF], vf[2][NF];
+    if (live) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const size_t at = block_base(kv, id[b], kvh, w0 + 32 * b);
+            const u32x4* kb = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.k) + at * (E4M3 ? 1 : 2));
+            // pieces of K: [piece][position]; a step takes two, one per lane half
+#pragma unroll
+            for (int x = 0; x < NF; ++x) kf[b][x] = stream_load(kb + (2 * x + lh) * 32 + lq);
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const size_t at = block_base(kv, id[b], kvh, w0 + 32 * b);
+            const u32x4* vb = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.v) + at * (E4M3 ? 1 : 2));
+            // pieces of V: [2t + h][j], or [h][j] with both t
+#pragma unroll
+            for (int x = 0; x < NF; ++x) vf[b][x] = stream_load(vb + (E4M3 ? lh * D + x * 32 : (2 * (x / DB) + lh) * D + (x % DB) * 32) + lq);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (a.rope.tab) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float c = cs[e >> 1][2 * (e & 1)], sn = cs[e >> 1][2 * (e & 1) + 1];
+            const float x = (float)qlo[e], y = (float)qhi[e];
+            qlo[e] = (bf16)(x * c - y * sn);
+            qhi[e] = (bf16)(y * c + x * sn);
+        }
+    }
+    if (tid < units) {
+        *reinterpret_cast<bf16x8*>(&qs[ur][uj]) = qlo;
+        *reinterpret_cast<bf16x8*>(&qs[ur][D / 2 + uj]) = qhi;
+    }
+    // hand-over through LDS; a full barrier would drain the stream
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+
+    if (live) {
+        const int qr = lq < rows ? lq : 0;                   // columns past the rows repeat the first and are dropped
+        const int qpos = before + (r0 + qr) / G;
+        f32x16 sacc[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[b][r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            // e4m3: step 2x + y takes bytes 8y.. of piece pair x, dims 32x + 16h + 8y ..
+            const int j = E4M3 ? (ks >> 1) * 32 + lh * 16 + (ks & 1) * 8 : ks * 16 + lh * 8;
+            const bf16x8 qf = *reinterpret_cast<const bf16x8*>(&qs[qr][j]);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                bf16x8 kk;
+                if (E4M3) kk = e4m3_to_bf16(kf[b][ks >> 1][2 * (ks & 1)], kf[b][ks >> 1][2 * (ks & 1) + 1]);
+                else kk = *reinterpret_cast<const bf16x8*>(&kf[b][ks]);
+                sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf, sacc[b], 0, 0, 0);
+            }
+        }
+        // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
+        const int p_min = before + r0 / G, p_max = before + (r0 + rows - 1) / G;
+        if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !there[0] || !there[1]) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int pos = w0 + b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+                    const bool seen = there[b] && pos <= qpos && (!a.window || pos > qpos - a.window);
+                    sacc[b][r] = seen ? sacc[b][r] : -INFINITY;
+                }
+            if (w0 + 64 > hi || w0 < lo || !there[0] || !there[1]) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    auto keep = [&](int off) {               // offset inside the block, lane half left out
+                        const int pos = w0 + 32 * b + off + 4 * lh;
+                        return there[b] && pos >= lo && pos < hi;
+                    };
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {        // positions 16 t + 8 g + 4 lh + 0..3
+                            const int off = 16 * t + 8 * g;
+                            if (E4M3) {
+                                const uint32_t m = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) | (keep(off + 2) ? 0xff0000u : 0) |
+                                                   (keep(off + 3) ? 0xff000000u : 0);
+#pragma unroll
+                                for (int x = 0; x < NF; ++x) vf[b][x][2 * t + g] &= m;
+                            } else {
+                                const uint32_t m0 = (keep(off) ? 0xffffu : 0) | (keep(off + 1) ? 0xffff0000u : 0);
+                                const uint32_t m1 = (keep(off + 2) ? 0xffffu : 0) | (keep(off + 3) ? 0xffff0000u : 0);
+#pragma unroll
+                                for (int db = 0; db < DB; ++db) {
+                                    vf[b][t * DB + db][2 * g] &= m0;
+                                    vf[b][t * DB + db][2 * g + 1] &= m1;
+                                }
+                            }
+                        }
+                }
+            }
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) m = fmaxf(m, sacc[b][r]);
+        m = fmaxf(m, __shfl_xor(m, 32, kWave)) * a.scale_log2;   // scale > 0
+        const float ref = finite_or_0(m);
+        float l = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
+                sacc[b][r] = p;
+                l += p;
+            }
+        l += __shfl_xor(l, 32, kWave);
+        f32x16 oacc[DB];
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                bf16x8 pf;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[e] = (bf16)sacc[b][8 * t + e];
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    bf16x8 vv;
+                    if (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
+                    else vv = *reinterpret_cast<const bf16x8*>(&vf[b][t * DB + db]);
+                    oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
+                }
+            }
+        if (lq < rows) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r4 = 0; r4 < 4; ++r4)
+                    *reinterpret_cast<float4*>(&osh[wave][lq][db * 32 + 8 * r4 + 4 * lh]) =
+                        make_float4(oacc[db][4 * r4], oacc[db][4 * r4 + 1], oacc[db][4 * r4 + 2], oacc[db][4 * r4 + 3]);
+            if (lh == 0) {
+                wmx[wave][lq] = m;
+                wsum[wave][lq] = l;
+            }
+        }
+    } else {
+        for (int x = lane; x < rows * D; x += 64) osh[wave][x / D][x % D] = 0.f;
+        if (lane < rows) {
+            wmx[wave][lane] = -INFINITY;
+            wsum[wave][lane] = 0.f;
+        }
+    }
+    __syncthreads();
+    const bool alone = hi - (lo & ~63) <= CH;                // the only chunk: the output itself
+    for (int x = tid; x < rows * D; x += 256) {
+        const int g = x / D, dd = x - g * D;
+        const float M = fmaxf(fmaxf(wmx[0][g], wmx[1][g]), fmaxf(wmx[2][g], wmx[3][g]));
+        const float ref = finite_or_0(M);
+        float acc = 0.f, L = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float f = exp2f(wmx[v][g] - ref);
+            acc = fmaf(osh[v][g][dd], f, acc);
+            L = fmaf(wsum[v][g], f, L);
+        }
+        const int t = (r0 + g) / G, head = kvh * G + (r0 + g) - t * G;
+        if (alone) {
+            a.out[(size_t)(q0 + t) * a.out_stride + head * D + dd] = (bf16)(L > 0.f ? acc / L * kv.v_scale : 0.f);
+        } else {
+            float* pp = partial + partial_at(w, bv.n_decode, i, t, a.Hq, head, chunk, D);
+            pp[dd] = acc;
+            if (dd == 0) {
+                pp[D] = M;
+                pp[D + 1] = L;
+            }
+        }
+    }
+}
+
+// Joins the chunks of the narrow sequences that have several, in increasing order: one workgroup per (token, query head), one
+// thread per head dim, sixteen chunks' loads in flight at once.
+template <int D>
+__global__ __launch_bounds__(D) void paged_narrow_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
+                                                              const float* __restrict__ partial) {
+    constexpr int NB = 16;
+    int i = blockIdx.x, token = 0;
+    if (i >= bv.n_decode) {
+        const int x = i - bv.n_decode;
+        i = bv.n_decode + x / w.short_tokens;
+        token = x % w.short_tokens;
+    }
+    const int h = blockIdx.y, dd = threadIdx.x;
+    const int s = bv.decode_seqs[i];
+    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
+    if (token >= n) return;
+    int nch = (before + n - (first_seen(before, a.window) & ~63) + kDecodeChunk - 1) / kDecodeChunk;
+    if (nch == 1) return;                                    // the output is there
+    if (nch > w.max_chunks) nch = w.max_chunks;
+    const float* base = partial + partial_at(w, bv.n_decode, i, token, a.Hq, h, 0, D);
+    float M = -INFINITY, num = 0.f, den = 0.f;
+    for (int c0 = 0; c0 < nch; c0 += NB) {
+        float mv[NB], ov[NB], lv[NB];
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const float* pc = base + (size_t)(c0 + u < nch ? c0 + u : nch - 1) * (D + 2);
+            mv[u] = pc[D];
+            ov[u] = pc[dd];
+            lv[u] = pc[D + 1];
+        }
+        float Mb = M;
+#pragma unroll
+        for (int u = 0; u < NB; ++u) Mb = fmaxf(Mb, mv[u]);
+        const float ref = finite_or_0(Mb), keep = exp2f(M - ref);
+        num *= keep;
+        den *= keep;
+        M = Mb;
+        // no branches: behind one every load would be waited for by itself.  A chunk past the end gets weight zero.
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const float f = c0 + u < nch ? exp2f(mv[u] - ref) : 0.f;
+            num = fmaf(ov[u], f, num);
+            den = fmaf(lv[u], f, den);
+        }
+    }
+    a.out[(size_t)(q0 + token) * a.out_stride + h * D + dd] = (bf16)(den > 0.f ? num / den * kv.v_scale : 0.f);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Wide: 128 rows per workgroup, 32 per wave, keys in tiles of 64 through LDS.  S^T = K Q^T, so that a lane pair (lane, lane + 32)
+// owns a row: its maximum and sum need one exchange, the rescale of O^T is a per-lane factor, and P^T goes from the score
+// accumulators into O^T = V^T P^T without leaving registers, since V's pieces hold the positions in the accumulators' order.
+// Activation caches move global -> LDS by DMA, the next tile's loads between the score products; e4m3 goes through registers, where it
+// becomes bf16, one tile ahead.  Bound by the vector pipe (32 exponentials per lane and tile) and the matrix pipe.
+// ---------------------------------------------------------------------------------------------
+struct WideUnit {
+    int item, sub, split, kvh;
+};
+// XCD-aware: workgroups go to the eight XCDs in turn; with a multiple of eight kv heads each XCD takes whole kv heads and walks
+// one after the other, longest key ranges first, so that what runs on it at a time shares the K and V in its L2.
+__device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int G, int Hkv, int splits) {
+    const int per_head = n_items * G * splits;
+    WideUnit u;
+    int rest;
+    if ((Hkv & 7) == 0) {
+        const int seq = b >> 3, k = seq / per_head;
+        u.kvh = (b & 7) * (Hkv >> 3) + k;
+        rest = seq - k * per_head;
+    } else {
+        u.kvh = b / per_head;
+        rest = b - u.kvh * per_head;
+    }
+    u.item = rest / (G * splits);
+    rest -= u.item * (G * splits);
+    u.sub = G - 1 - rest / splits;
+    u.split = rest % splits;
+    return u;
+}
+
+// the tiles of 64 keys that rows r0 .. r0 + 127 see, or the range of them that `split` names
+struct WideKeys {
+    int t0, t1, splits;
+};
+__device__ __forceinline__ WideKeys wide_keys(int before, int r0, int R, int G, int window, int split, int splits) {
+    const int first = before + r0 / G, last = before + (r0 + kWideRows < R ? r0 + kWideRows - 1 : R - 1) / G;
+    WideKeys k;
+    k.t0 = first_seen(first, window) >> 6;
+    k.t1 = (last >> 6) + 1;
+    const int per = (k.t1 - k.t0 + splits - 1) / splits;
+    k.splits = (k.t1 - k.t0 + per - 1) / per;
+    k.t0 += split * per;
+    if (k.t0 + per < k.t1) k.t1 = k.t0 + per;
+    return k;
+}
+
+template <int D, bool E4M3, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
+                                                            float* __restrict__ partial) {
+    constexpr int DB = D / 32, KS = D / 16, BLK = 32 * D;
+    constexpr int NL = D / 32;           // 1 KiB DMA loads per wave and tile, of K and again of V
+    constexpr int NC = D / 64;           // e4m3: 16-byte loads per thread and tile, of K and again of V
+    constexpr int STAGE = 4 * BLK;       // K tile (two blocks), V tile (two blocks)
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    bf16* smem = reinterpret_cast<bf16*>(smem_raw);
+
+    const int Hkv = kv.Hkv, G = a.Hq / Hkv;
+    const WideUnit unit = wide_unit(blockIdx.x, bv.n_prefill_items, G, Hkv, w.splits);
+    const int s = bv.prefill_items[2 * unit.item], qt = bv.prefill_items[2 * unit.item + 1];
+    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s], row = bv.seq_slot[s];
+    const int R = n * G, r0 = (qt * G + unit.sub) * kWideRows;
+    if (r0 >= R || R <= w.narrow_limit) return;
+    const WideKeys keys = wide_keys(before, r0, R, G, a.window, unit.split, w.splits);
+    if (SPLIT && keys.t0 >= keys.t1) return;
+    const int hi = before + n, lo = first_seen(before + r0 / G, a.window);
+    const int kvh = unit.kvh;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lq = lane & 31, lh = lane >> 5;
+    const int r = r0 + wave * 32 + lq;
+    const bool valid = r < R;
+    const int rc = valid ? r : R - 1, token = rc / G, head = kvh * G + rc - token * G, qpos = before + token;
+    const int wr = r0 + wave * 32 < R - 1 ? r0 + wave * 32 : R - 1, wl = r0 + wave * 32 + 31 < R - 1 ? r0 + wave * 32 + 31 : R - 1;
+    const int wave_min_pos = before + wr / G, wave_max_pos = before + wl / G;
+
+    // A tile's two blocks: their page, 0 in place of one that is not there.
+    struct Tile {
+        int id[2];
+        bool there[2];
+    };
+    auto look_up = [&](int tile) {
+        Tile t;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int pos = tile * 64 + 32 * b;
+            t.id[b] = pos < hi ? page_of(kv, row, pos) : -1;
+            t.there[b] = t.id[b] >= 0;
+            if (!t.there[b]) t.id[b] = 0;
+        }
+        return t;
+    };
+    // this wave's block of a tile: waves 0 and 1 move the first, 2 and 3 the second
+    const int wblk = wave >> 1;
+    auto source = [&](const Tile& t, int tile) { return block_base(kv, wblk ? t.id[1] : t.id[0], kvh, tile * 64 + 32 * wblk); };
+    auto issue_one = [&](size_t src, int stage, int q) {
+        bf16* st = smem + stage * STAGE;
+        const int piece = wave * NL + q % NL;                // 512 elements each
+        const size_t at = src + (size_t)(piece % (BLK / 512)) * 512 + lane * 8;
+        if (q < NL) __builtin_amdgcn_global_load_lds((gptr_t)(static_cast<const bf16*>(kv.k) + at), (lptr_t)(st + piece * 512), 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((gptr_t)(static_cast<const bf16*>(kv.v) + at), (lptr_t)(st + 2 * BLK + piece * 512), 16, 0, 0);
+    };
+    u32x4 kreg[NC], vreg[NC];
+    auto fetch = [&](const Tile& t, int tile) {              // e4m3
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + 256 * i, blk = NC == 2 ? i : wblk, in = c - blk * (2 * D);
+            const size_t at = block_base(kv, blk ? t.id[1] : t.id[0], kvh, tile * 64 + 32 * blk) + in * 16;
+            kreg[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.k) + at);
+            vreg[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.v) + at);
+        }
+    };
+    auto unpack = [&](int stage) {
+        bf16* ks = smem + stage * STAGE;
+        bf16* vs = ks + 2 * BLK;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + 256 * i, blk = NC == 2 ? i : wblk, in = c - blk * (2 * D);
+            const int piece = in >> 5, p = in & 31, h = in / D, j = in - h * D;
+            *reinterpret_cast<bf16x8*>(ks + blk * BLK + ((2 * piece) * 32 + p) * 8) = e4m3_to_bf16(kreg[i][0], kreg[i][1]);
+            *reinterpret_cast<bf16x8*>(ks + blk * BLK + ((2 * piece + 1) * 32 + p) * 8) = e4m3_to_bf16(kreg[i][2], kreg[i][3]);
+            *reinterpret_cast<bf16x8*>(vs + blk * BLK + (h * D + j) * 8) = e4m3_to_bf16(vreg[i][0], vreg[i][1]);
+            *reinterpret_cast<bf16x8*>(vs + blk * BLK + ((2 + h) * D + j) * 8) = e4m3_to_bf16(vreg[i][2], vreg[i][3]);
+        }
+    };
+
+    Tile now = look_up(keys.t0), next = now;
+    if (E4M3) {
+        fetch(now, keys.t0);
+        unpack(0);
+    } else {
+        const size_t src = source(now, keys.t0);
+#pragma unroll
+        for (int q = 0; q < 2 * NL; ++q) issue_one(src, 0, q);
+    }
+
+    bf16x8 qf[KS];
+    {
+        const bf16* qp = a.q + (size_t)(q0 + token) * a.q_stride + head * D;
+        const float* cs = a.rope.tab ? rope_row(a.rope, qpos, D) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < KS / 2; ++ks) rotate8(qp + ks * 16 + lh * 8, cs ? cs + 2 * (ks * 16 + lh * 8) : nullptr, D / 2, qf[ks], qf[ks + KS / 2]);
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[b][x] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    if (keys.t0 + 1 < keys.t1) next = look_up(keys.t0 + 1);
+
+    for (int tile = keys.t0; tile < keys.t1; ++tile) {
+        const int stage = (tile - keys.t0) & 1, kbase = tile * 64;
+        __builtin_amdgcn_s_waitcnt(0x0070);                  // own pieces of this tile landed, own LDS accesses done
+        __syncthreads();                                     // everyone's; the other stage is free
+        const bf16* Ks = smem + stage * STAGE;
+        const bf16* Vs = Ks + 2 * BLK;
+        const Tile cur = now;
+        // after the last tile it is requested once more into the idle stage: no branch between the products
+        const int nt = tile + 1 < keys.t1 ? tile + 1 : tile;
+        now = tile + 1 < keys.t1 ? next : now;
+        if (tile + 2 < keys.t1) next = look_up(tile + 2);
+        const size_t src = source(now, nt);
+        if (E4M3) fetch(now, nt);
+        if (kbase + 64 > hi || kbase < lo || !cur.there[0] || !cur.there[1]) {     // workgroup-uniform
+            // values that nobody may see: one thread per 8 positions of a head dim
+            bf16* vw = smem + stage * STAGE + 2 * BLK;
+            for (int c = tid; c < 8 * D; c += 256) {
+                const int blk = c / (4 * D), piece = (c / D) & 3;
+                const int p = kbase + 32 * blk + 16 * (piece >> 1) + 4 * (piece & 1);
+                bf16x8 v = *reinterpret_cast<bf16x8*>(vw + c * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int pos = p + (e & 3) + 8 * (e >> 2);
+                    if (!(blk ? cur.there[1] : cur.there[0]) || pos < lo || pos >= hi) v[e] = (bf16)0.f;
+                }
+                *reinterpret_cast<bf16x8*>(vw + c * 8) = v;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        }
+        // nothing for this wave: behind its rows, or before their windows
+        if (kbase > wave_max_pos || (a.window && kbase + 63 <= wave_min_pos - a.window)) {
+            if (!E4M3)
+#pragma unroll
+                for (int q = 0; q < 2 * NL; ++q) issue_one(src, stage ^ 1, q);
+        } else {
+            f32x16 sacc[2];
+            // operand fetch runs ahead of the products by hand: each K fragment of the first key block is replaced by the second
+            // block's when its product has gone, and under the second block's the first V fragments are requested
+            constexpr int EVERY = (2 * KS) / (2 * NL);
+            auto k_frag = [&](int kb, int ks) { return *reinterpret_cast<const bf16x8*>(&Ks[kb * BLK + ((ks * 2 + lh) * 32 + lq) * 8]); };
+            auto v_frag = [&](int t, int b) {
+                return *reinterpret_cast<const bf16x8*>(&Vs[(t >> 1) * BLK + ((2 * (t & 1) + lh) * D + b * 32 + lq) * 8]);
+            };
+            bf16x8 ka[KS], vfr[2][DB];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) ka[ks] = k_frag(0, ks);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) sacc[kb][x] = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], sacc[kb], 0, 0, 0);
+                    if (kb == 0) ka[ks] = k_frag(1, ks);
+                    else if (ks < 2 * DB) vfr[ks / DB][ks % DB] = v_frag(ks / DB, ks % DB);
+                    const int step = kb * KS + ks;
+                    if (!E4M3 && step % EVERY == EVERY - 1) issue_one(src, stage ^ 1, step / EVERY);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if (kbase + 63 > wave_min_pos || (a.window && kbase <= wave_max_pos - a.window) || !cur.there[0] || !cur.there[1]) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const int pos = kbase + kb * 32 + 8 * (x >> 2) + 4 * lh + (x & 3);
+                        const bool seen = cur.there[kb] && pos <= qpos && (!a.window || pos > qpos - a.window);
+                        sacc[kb][x] = seen ? sacc[kb][x] : -INFINITY;
+                    }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sacc[kb][x]);
+            mx = fmaxf(m, mx * a.scale_log2);                // scale > 0
+            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            const float ref = finite_or_0(mx);
+            if (__builtin_amdgcn_ballot_w64(mx != m) != 0) { // some row's maximum moved
+                const float alpha = exp2_flush(m - ref);
+                l *= alpha;
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[b][x] *= alpha;
+                m = mx;
+            }
+            float rs = 0.f;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const float p = exp2_flush(fmaf(sacc[kb][x], a.scale_log2, -ref));
+                    sacc[kb][x] = p;
+                    rs += p;
+                }
+            rs += __shfl_xor(rs, 32, kWave);
+            l += rs;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                bf16x8 pf;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[e] = (bf16)sacc[t >> 1][8 * (t & 1) + e];
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[t & 1][b], pf, o[b], 0, 0, 0);
+                    if (t + 2 < 4) vfr[t & 1][b] = v_frag(t + 2, b);
+                }
+            }
+        }
+        if (E4M3) unpack(stage ^ 1);
+    }
+
+    __builtin_amdgcn_s_waitcnt(0x0070);                      // no LDS write may be in flight when the workgroup ends
+    if (SPLIT) {
+        float* base = partial + ((((size_t)unit.item * G + unit.sub) * Hkv + kvh) * w.splits + unit.split) * (kWideRows * (D + 2));
+        float* op = base + wave * 32 * D + lq * 4;           // [dims by fours][row][4]
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4)
+                *reinterpret_cast<float4*>(op + ((b * 4 + r4) * 2 + lh) * 128) =
+                    make_float4(o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]);
+        if (lh == 0) *reinterpret_cast<float2*>(base + kWideRows * D + (wave * 32 + lq) * 2) = make_float2(m, l);
+    } else if (valid) {
+        const float inv = l > 0.f ? kv.v_scale / l : 0.f;
+        bf16* op = a.out + (size_t)(q0 + token) * a.out_stride + head * D;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                bf16x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[b][r4 * 4 + e] * inv);
+                *reinterpret_cast<bf16x4*>(op + b * 32 + 8 * r4 + 4 * lh) = v;
+            }
+    }
+}
+
+// Joins the key ranges of wide rows, in increasing order: one workgroup per 32 rows.
+template <int D>
+__global__ __launch_bounds__(256) void paged_wide_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
+                                                              const float* __restrict__ partial) {
+    const int Hkv = kv.Hkv, G = a.Hq / Hkv;
+    const int part = blockIdx.x & 3, b = blockIdx.x >> 2;
+    const int kvh = b % Hkv, sub = b / Hkv % G, item = b / Hkv / G;
+    const int s = bv.prefill_items[2 * item], qt = bv.prefill_items[2 * item + 1];
+    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
+    const int R = n * G, r0 = (qt * G + sub) * kWideRows;
+    const int x = part * 32 + (threadIdx.x & 31), r = r0 + x;
+    if (r >= R || R <= w.narrow_limit) return;
+    const WideKeys keys = wide_keys(before, r0, R, G, a.window, 0, w.splits);
+    const float* base = partial + (((size_t)item * G + sub) * Hkv + kvh) * w.splits * (kWideRows * (D + 2));
+    constexpr size_t UNIT = kWideRows * (D + 2);
+    float M = -INFINITY;
+    for (int k = 0; k < keys.splits; ++k) M = fmaxf(M, base[k * UNIT + kWideRows * D + x * 2]);
+    const float ref = finite_or_0(M);
+    constexpr int NQ = D / 32;
+    float4 acc[NQ] = {};
+    float L = 0.f;
+    for (int k = 0; k < keys.splits; ++k) {
+        const float* pk = base + k * UNIT;
+        const float2 ml = *reinterpret_cast<const float2*>(pk + kWideRows * D + x * 2);
+        const float f = exp2f(ml.x - ref);
+        L = fmaf(ml.y, f, L);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(pk + part * 32 * D + (i * 8 + (threadIdx.x >> 5)) * 128 + (threadIdx.x & 31) * 4);
+            acc[i].x = fmaf(v.x, f, acc[i].x);
+            acc[i].y = fmaf(v.y, f, acc[i].y);
+            acc[i].z = fmaf(v.z, f, acc[i].z);
+            acc[i].w = fmaf(v.w, f, acc[i].w);
+        }
+    }
+    const float inv = L > 0.f ? kv.v_scale / L : 0.f;
+    const int token = r / G, head = kvh * G + r - token * G;
+    bf16* op = a.out + (size_t)(q0 + token) * a.out_stride + head * D + (threadIdx.x >> 5) * 4;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const bf16x4 v = {(bf16)(acc[i].x * inv), (bf16)(acc[i].y * inv), (bf16)(acc[i].z * inv), (bf16)(acc[i].w * inv)};
+        *reinterpret_cast<bf16x4*>(op + i * 32) = v;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+static size_t narrow_bytes(const PagedWork& w, const BatchView& bv, int Hq, int d) {
+    if (w.max_chunks <= 1) return 0;
+    const size_t tokens = (size_t)bv.n_decode + (size_t)w.n_short * w.short_tokens;
+    return (tokens * Hq * w.max_chunks * (d + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, int, int d) {
+    const size_t wide = w.splits > 1 ? (size_t)bv.n_prefill_items * Hq * w.splits * kWideRows * (d + 2) * sizeof(float) : 0;
+    return narrow_bytes(w, bv, Hq, d) + wide;
+}
+
+template <int D, bool E4M3, bool SPLIT>
+static void launch_wide(const PagedQuery& q, const PagedWork& w, const BatchView& bv, const PagedView& kv, float* ws, hipStream_t st) {
+    constexpr int kLds = 2 * 4 * 32 * D * (int)sizeof(bf16);             // two stages of a K and a V tile
+    static LdsLimit limit;
+    (void)limit.raise(reinterpret_cast<const void*>(paged_wide_kernel<D, E4M3, SPLIT>), kLds);
+    hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, SPLIT>), dim3((unsigned)(bv.n_prefill_items * q.Hq * w.splits)), dim3(256), kLds, st, q,
+                       w, bv, kv, ws);
+    if (SPLIT) hipLaunchKernelGGL(paged_wide_join_kernel<D>, dim3((unsigned)(bv.n_prefill_items * q.Hq * 4)), dim3(256), 0, st, q, w, bv, kv, ws);
+}
+
+template <int D, bool E4M3>
+static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView& bv, const PagedView& kv, float* ws, hipStream_t st) {
+    const int n_narrow = bv.n_decode + w.n_short;
+    if (n_narrow > 0) {
+        constexpr int WAVES = E4M3 ? 3 : D == 128 ? 2 : 4;
+        const unsigned grid = (unsigned)((w.list + (n_narrow - w.first) * w.chunks) * kv.Hkv * w.col_tiles);
+        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, WAVES> : paged_narrow_kernel<D, E4M3, kNarrowRows, 2>;
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
+        if (w.max_chunks > 1) {
+            const unsigned tokens = (unsigned)(bv.n_decode + w.n_short * w.short_tokens);
+            hipLaunchKernelGGL(paged_narrow_join_kernel<D>, dim3(tokens, q.Hq), dim3(D), 0, st, q, w, bv, kv, ws);
+        }
+    }
+    if (w.wide_units > 0) {
+        float* wide = ws ? ws + narrow_bytes(w, bv, q.Hq, D) / sizeof(float) : nullptr;
+        (w.splits > 1 ? launch_wide<D, E4M3, true> : launch_wide<D, E4M3, false>)(q, w, bv, kv, wide, st);
+    }
+}
+
+void launch_paged_attention(const PagedQuery& q, const PagedWork& w, bool e4m3, const BatchView& bv, const PagedView& kv, float* ws,
+                            hipStream_t st) {
+    auto go = kv.d == 128 ? (e4m3 ? launch_all<128, true> : launch_all<128, false>) : (e4m3 ? launch_all<64, true> : launch_all<64, false>);
+    go(q, w, bv, kv, ws, st);
+}
+
+#else  // BZ_FP32_DEBUG
+// ---------------------------------------------------------------------------------------------
+// fp32 debug build: one wave per (token, query head), 64 positions at a time with a running maximum and sum; a lane scores one
+// position and owns d / 64 dims of the output.
+// ---------------------------------------------------------------------------------------------
+template <bool E4M3, int D>
+__global__ __launch_bounds__(64) void paged_attn_plain_kernel(PagedQuery a, BatchView bv, PagedView kv) {
+    __shared__ float qs[D];
+    const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
+    const int s = bv.token_seq[t], row = bv.seq_slot[s];
+    const int pos = bv.kv_before[s] + (t - bv.q_start[s]);
+    const int kvh = h / (a.Hq / kv.Hkv);
+    const act_t* q = a.q + (size_t)t * a.q_stride + h * D;
+    for (int j = lane; j < D / 2; j += 64) {
+        const float lo = to_f32(q[j]), hi = to_f32(q[D / 2 + j]);
+        float o_lo = lo, o_hi = hi;
+        if (a.rope.tab) {
+            const float* cs = rope_row(a.rope, pos, D);
+            o_lo = lo * cs[2 * j] - hi * cs[2 * j + 1];
+            o_hi = hi * cs[2 * j] + lo * cs[2 * j + 1];
+        }
+        act_t r;
+        from_f32(r, o_lo);
+        qs[j] = to_f32(r);
+        from_f32(r, o_hi);
+        qs[D / 2 + j] = to_f32(r);
+    }
+    __syncthreads();
+    const int first = a.window && pos + 1 > a.window ? pos + 1 - a.window : 0;
+    float m = -INFINITY, l = 0.f, o[D / 64] = {};
+    for (int c0 = first & ~63; c0 <= pos; c0 += 64) {
+        const int kp = c0 + lane;
+        const int id = kp <= pos && kp >= first ? page_of(kv, row, kp) : -1;
+        float sc = -INFINITY;
+        if (id >= 0) {
+            const size_t at = block_base(kv, id, kvh, kp);
+            float x = 0.f;
+            for (int j = 0; j < D; ++j) x = fmaf(qs[j], cache_get<E4M3>(kv.k, at + k_block_offset<E4M3>(kp & 31, j)), x);
+            sc = x * a.scale_log2;
+        }
+        const float mx = fmaxf(m, wave_max(sc));
+        if (mx == -INFINITY) continue;                       // nothing seen yet; wave-uniform
+        const float alpha = exp2f(m - mx), w = exp2f(sc - mx);
+        m = mx;
+        l = l * alpha + wave_sum(w);
+        for (int i = 0; i < D / 64; ++i) o[i] *= alpha;
+        const int n = pos + 1 - c0 < 64 ? pos + 1 - c0 : 64;
+        for (int u = 0; u < n; ++u) {
+            const int uid = __shfl(id, u, 64);
+            if (uid < 0) continue;
+            const float wu = __shfl(w, u, 64);
+            const size_t at = block_base(kv, uid, kvh, c0 + u);
+            for (int i = 0; i < D / 64; ++i)
+                o[i] = fmaf(wu, cache_get<E4M3>(kv.v, at + v_block_offset<E4M3>((c0 + u) & 31, lane + 64 * i, D)), o[i]);
+        }
+    }
+    for (int i = 0; i < D / 64; ++i)
+        from_f32(a.out[(size_t)t * a.out_stride + h * D + lane + 64 * i], l > 0.f ? o[i] / l * kv.v_scale : 0.f);
+}
+
+size_t paged_attention_bytes(const PagedWork&, const BatchView&, int, int, int) { return 0; }
+
+void launch_paged_attention(const PagedQuery& a, const PagedWork&, bool e4m3, const BatchView& bv, const PagedView& kv, float*,
+                            hipStream_t st) {
+    auto kern = kv.d == 128 ? (e4m3 ? paged_attn_plain_kernel<true, 128> : paged_attn_plain_kernel<false, 128>)
+                            : (e4m3 ? paged_attn_plain_kernel<true, 64> : paged_attn_plain_kernel<false, 64>);
+    hipLaunchKernelGGL(kern, dim3(bv.T, a.Hq), dim3(64), 0, st, a, bv, kv);
+}
+#endif
+
+}  // namespace bz

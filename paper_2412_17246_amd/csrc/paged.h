@@ -42,7 +42,9 @@ __host__ __device__ inline int v_block_offset(int p, int j, int d) {
 __device__ __forceinline__ int page_of(const PagedView& kv, int row, int pos) {
     const int i = pos >> kv.page_shift;
     if (i >= kv.per_row) return -1;
-    const int id = kv.table[(size_t)row * kv.per_row + i];
+    // through the constant address space: a scalar load where the position is uniform, also behind stores and barriers
+    typedef const __attribute__((address_space(4))) int32_t* entry_t;
+    const int id = *(entry_t)(uintptr_t)(kv.table + (size_t)row * kv.per_row + i);
     return id >= 0 && id < kv.n_pages ? id : -1;
 }
 // First element of the block of 32 positions that holds `pos`, in page `id`, of kv head `head`.
@@ -90,9 +92,22 @@ struct PagedQuery {
     int Hq, window;
     float scale_log2;          // score scale times log2 e, and times what 1 in the K cache stands for
 };
-// What the attention of a batch needs to know of its lengths, from the host's copy of them.
+// How the attention of a batch is cut, from the host's copy of its lengths.  A sequence's new tokens times the query heads of a
+// kv head are its rows there.  Narrow: single new tokens, and sequences of few rows; a workgroup takes up to kNarrowRows of them
+// over one chunk of kDecodeChunk positions.  Wide: a workgroup takes kWideRows rows over the keys they see, or over one of
+// `splits` ranges of them.
+constexpr int kNarrowRows = 32, kWideRows = 128;
 struct PagedWork {
-    int dummy;
+    int n_short, short_tokens; // sequences of several tokens that are narrow (the first of BatchView::short_seqs), their most tokens
+    int list;                  // workgroups of single tokens that the batch's work list names (no window), for one kv head
+    int first;                 // sequences of decode_seqs and short_seqs from here on have `chunks` workgroups each per kv head
+    int chunks;
+    int max_chunks;            // of any narrow sequence
+    int col_tiles;             // tiles of kNarrowRows rows of a narrow sequence
+    int narrow_rows;           // most rows of one
+    int narrow_limit;          // most rows of a sequence of several tokens that is narrow
+    int wide_units;            // workgroups of wide rows that have work, times kv heads and ranges
+    int splits;
 };
 size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, int Hkv, int d);
 void launch_paged_attention(const PagedQuery& q, const PagedWork& w, bool e4m3, const BatchView& bv, const PagedView& kv,

@@ -1,6 +1,8 @@
 // Host side of the paged KV cache's operations: argument checks and launches.
 #include <math.h>
 
+#include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "instance.h"
@@ -62,6 +64,44 @@ int lengths_ok(const bz_batch* b, const bz_paged_kv* kv, const float* rope, int 
     return BZ_OK;
 }
 
+int chunks_of(int64_t keys) { return (int)((keys + kDecodeChunk - 1) / kDecodeChunk); }
+
+// keys that the tokens of a sequence see between them, from a multiple of 64 on
+int64_t keys_of(int64_t before, int64_t n, int window) {
+    const int64_t lo = window && before + 1 > window ? (before + 1 - window) & ~(int64_t)63 : 0;
+    return before + n - lo;
+}
+
+PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int window) {
+    PagedWork w{};
+    const int G = Hq / Hkv;
+    int64_t most = 0;
+    w.narrow_limit = b->short_qlen.empty() ? 0 : kNarrowRows;       // a batch in tight storage has no list of them
+    while (w.n_short < (int)b->short_qlen.size() && b->short_qlen[w.n_short] * G <= kNarrowRows) ++w.n_short;
+    w.short_tokens = w.n_short ? b->short_qlen[w.n_short - 1] : 0;
+    for (int i = 0; i < w.n_short; ++i) most = std::max(most, keys_of(b->kv_before[b->short_seqs[i]], b->short_qlen[i], window));
+    if (window)
+        for (int s : b->decode_seqs) most = std::max(most, keys_of(b->kv_before[s], 1, window));
+    w.list = window ? 0 : bv.n_decode_work;
+    w.first = window ? 0 : bv.n_decode;
+    w.chunks = chunks_of(most);
+    w.max_chunks = std::max(w.chunks, window ? 0 : bv.decode_chunks);
+    w.col_tiles = (std::max(G, 1) + kNarrowRows - 1) / kNarrowRows;
+    w.narrow_rows = std::max(std::min(G, kNarrowRows), w.short_tokens * G);
+    // wide rows: enough ranges of the keys that the chip is full, of four tiles of 64 keys at least
+    int64_t units = 0, keys = 0;
+    for (int s = 0; s < b->B; ++s) {
+        const int n = b->q_start[s + 1] - b->q_start[s];
+        if (n < 2 || n * G <= w.narrow_limit) continue;
+        const int64_t rows = (int64_t)n * G;
+        units += (rows + kWideRows - 1) / kWideRows * Hkv;
+        keys = std::max(keys, keys_of((int64_t)b->kv_before[s] + n - std::min<int64_t>(n, kWideRows / G + 1), std::min<int64_t>(n, kWideRows / G + 1), window));
+    }
+    w.splits = units ? (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / units, 16), keys / 256)) : 1;
+    w.wide_units = (int)std::min<int64_t>(units, 0x7fffffff);
+    return w;
+}
+
 int launched(const bz_batch* b, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "launch");
@@ -112,7 +152,8 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
 
 size_t bz_op_paged_attention_workspace_bytes(const bz_batch* batch, const bz_paged_kv* kv, int n_q_heads, int window) {
     if (!batch || !shape_ok(kv) || n_q_heads < 1 || n_q_heads % kv->n_kv_heads || n_q_heads > 1024 || window < 0) return 0;
-    return paged_attention_bytes(PagedWork{0}, batch_view(batch), n_q_heads, kv->n_kv_heads, kv->head_dim);
+    const BatchView bv = batch_view(batch);
+    return paged_attention_bytes(work_of(batch, bv, n_q_heads, kv->n_kv_heads, window), bv, n_q_heads, kv->n_kv_heads, kv->head_dim);
 }
 
 int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const void* q, int64_t q_stride, void* out,
@@ -127,8 +168,8 @@ int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const vo
     hipStream_t st = (hipStream_t)stream;
     int rc = lengths_ok(batch, kv, rope, rope_positions);
     if (rc) return rc;
-    const PagedWork work{0};
     const BatchView bv = batch_view(batch);
+    const PagedWork work = work_of(batch, bv, n_q_heads, kv->n_kv_heads, window);
     const size_t need = paged_attention_bytes(work, bv, n_q_heads, kv->n_kv_heads, kv->head_dim);
     if (need && (!workspace || workspace_bytes < need)) return BZ_ENOMEM;
     rc = batch_before_run(batch, st);
