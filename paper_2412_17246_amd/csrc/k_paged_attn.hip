@@ -15,7 +15,6 @@ namespace bz {
 #ifndef BZ_FP32_DEBUG
 namespace {
 
-typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -24,9 +23,6 @@ __device__ __forceinline__ float exp2_flush(float x) { return __builtin_amdgcn_e
 
 // reference of a running maximum that may not have seen a key yet
 __device__ __forceinline__ float finite_or_0(float m) { return m > -INFINITY ? m : 0.f; }
-
-template <class T>
-__device__ __forceinline__ T stream_load(const T* p) { return __builtin_nontemporal_load(p); }
 
 // eight e4m3 numbers to bf16, which holds each of them exactly
 __device__ __forceinline__ bf16x8 e4m3_to_bf16(uint32_t a, uint32_t b) {
@@ -76,28 +72,22 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     __shared__ float osh[4][RT][D];
     __shared__ __attribute__((aligned(16))) bf16 qs[RT][LD];
 
-    const int Hkv = kv.Hkv, G = a.Hq / Hkv;
-    const int listed = w.list * Hkv * w.col_tiles;
-    int i, s, row, kvh, ct, chunk;
-    if ((int)blockIdx.x < listed) {
-        const int per = Hkv * w.col_tiles, e = blockIdx.x / per;
+    const int G = w.by_group.d;
+    // kv heads next to each other, then chunks, then sequences: the order in which pages lie in memory
+    int e = w.by_heads.divide(blockIdx.x);
+    const int hc = blockIdx.x - e * w.by_heads.d, kvh = w.by_tiles.divide(hc), ct = hc - kvh * w.by_tiles.d;
+    int i, s, row, chunk;
+    if (e < w.list) {
         const int4 item = bv.decode_work[2 * e];
-        const int rest = blockIdx.x - per * bv.decode_work[2 * e + 1].x;
         s = item.x;
         row = item.y;
         i = item.z;
-        chunk = rest % item.w;
-        const int hc = rest / item.w;
-        kvh = hc / w.col_tiles;
-        ct = hc - kvh * w.col_tiles;
+        chunk = e - bv.decode_work[2 * e + 1].x;
     } else {
-        int rest = blockIdx.x - listed;
-        chunk = rest % w.chunks;
-        rest /= w.chunks;
-        ct = rest % w.col_tiles;
-        rest /= w.col_tiles;
-        kvh = rest % Hkv;
-        i = w.first + rest / Hkv;
+        e -= w.list;
+        i = w.by_chunks.divide(e);
+        chunk = e - i * w.by_chunks.d;
+        i += w.first;
         s = bv.decode_seqs[i];
         row = bv.seq_slot[s];
     }
@@ -105,7 +95,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     const int hi = before + n, lo = first_seen(before, a.window);
     const int c0 = (lo & ~63) + chunk * CH;
     const int r0 = ct * kNarrowRows, R = n * G;
-    if (c0 >= hi || r0 >= R || chunk >= w.max_chunks || kvh >= Hkv) return;
+    if (c0 >= hi || r0 >= R || chunk >= w.max_chunks) return;
     const int rows = R - r0 < RT ? R - r0 : RT;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -127,7 +117,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     const int units = rows * UPR;
     const int u = tid < units ? tid : units - 1;
     const int ur = u / UPR, uj = (u - ur * UPR) * 8;
-    const int ut = (r0 + ur) / G, uh = kvh * G + (r0 + ur) - ut * G;
+    const int ut = w.by_group.divide(r0 + ur), uh = kvh * G + (r0 + ur) - ut * G;
     const bf16* qp = a.q + (size_t)(q0 + ut) * a.q_stride + uh * D + uj;
     bf16x8 qlo = *reinterpret_cast<const bf16x8*>(qp), qhi = *reinterpret_cast<const bf16x8*>(qp + D / 2);
     f32x4 cs[4] = {};
@@ -140,21 +130,28 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 
     u32x4 kf[2][NF], vf[2][NF];
     if (live) {
+        // non-temporal: nobody reads them again.  A base in scalar registers, one vector register for all addresses of K, one for V.
+        constexpr int EL = E4M3 ? 1 : 2;
+        auto block = [&](void* cache, int b) {
+            return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(cache) + block_base(kv, id[b], kvh, w0 + 32 * b) * EL, 0,
+                                                     32 * D * EL, 0x00020000);
+        };
+        auto load = [&](__amdgpu_buffer_rsrc_t r, int lane_at, int at) {
+            return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 2));
+        };
+        // pieces of K: [piece][position]; a step takes two, one per lane half.  Pieces of V: [2t + h][j], or [h][j] with both t.
+        const int lane_k = (lh * 32 + lq) * 16, lane_v = (lh * D + lq) * 16;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const size_t at = block_base(kv, id[b], kvh, w0 + 32 * b);
-            const u32x4* kb = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.k) + at * (E4M3 ? 1 : 2));
-            // pieces of K: [piece][position]; a step takes two, one per lane half
+            const __amdgpu_buffer_rsrc_t r = block(kv.k, b);
 #pragma unroll
-            for (int x = 0; x < NF; ++x) kf[b][x] = stream_load(kb + (2 * x + lh) * 32 + lq);
+            for (int x = 0; x < NF; ++x) kf[b][x] = load(r, lane_k, x * 1024);
         }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const size_t at = block_base(kv, id[b], kvh, w0 + 32 * b);
-            const u32x4* vb = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.v) + at * (E4M3 ? 1 : 2));
-            // pieces of V: [2t + h][j], or [h][j] with both t
+            const __amdgpu_buffer_rsrc_t r = block(kv.v, b);
 #pragma unroll
-            for (int x = 0; x < NF; ++x) vf[b][x] = stream_load(vb + (E4M3 ? lh * D + x * 32 : (2 * (x / DB) + lh) * D + (x % DB) * 32) + lq);
+            for (int x = 0; x < NF; ++x) vf[b][x] = load(r, lane_v, E4M3 ? x * 512 : (x / DB) * (2 * D * 16) + (x % DB) * 512);
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -178,7 +175,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 
     if (live) {
         const int qr = lq < rows ? lq : 0;                   // columns past the rows repeat the first and are dropped
-        const int qpos = before + (r0 + qr) / G;
+        const int qpos = before + w.by_group.divide(r0 + qr);
         f32x16 sacc[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -198,27 +195,29 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
             }
         }
         // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
-        const int p_min = before + r0 / G, p_max = before + (r0 + rows - 1) / G;
+        const int p_min = before + w.by_group.divide(r0), p_max = before + w.by_group.divide(r0 + rows - 1);
         if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !there[0] || !there[1]) {
+            const int from = first_seen(qpos, a.window);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int pos = w0 + b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                    const bool seen = there[b] && pos <= qpos && (!a.window || pos > qpos - a.window);
-                    sacc[b][r] = seen ? sacc[b][r] : -INFINITY;
+                    const uint32_t reach = there[b] ? qpos - from + 1 : 0;
+                    sacc[b][r] = (uint32_t)(pos - from) < reach ? sacc[b][r] : -INFINITY;
+                    __builtin_amdgcn_sched_barrier(0);       // one at a time: 32 lane masks do not fit the scalar registers
                 }
             if (w0 + 64 > hi || w0 < lo || !there[0] || !there[1]) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    auto keep = [&](int off) {               // offset inside the block, lane half left out
-                        const int pos = w0 + 32 * b + off + 4 * lh;
-                        return there[b] && pos >= lo && pos < hi;
-                    };
+                    const uint32_t length = there[b] ? hi - lo : 0;
+                    auto keep = [&](int off) { return (uint32_t)(w0 + 32 * b + 4 * lh + off - lo) < length; };   // inside the block
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int g = 0; g < 2; ++g) {        // positions 16 t + 8 g + 4 lh + 0..3
+                        for (int g = 0; g < 2; ++g) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            // positions 16 t + 8 g + 4 lh + 0..3
                             const int off = 16 * t + 8 * g;
                             if (E4M3) {
                                 const uint32_t m = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) | (keep(off + 2) ? 0xff0000u : 0) |
@@ -307,7 +306,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
             acc = fmaf(osh[v][g][dd], f, acc);
             L = fmaf(wsum[v][g], f, L);
         }
-        const int t = (r0 + g) / G, head = kvh * G + (r0 + g) - t * G;
+        const int t = w.by_group.divide(r0 + g), head = kvh * G + (r0 + g) - t * G;
         if (alone) {
             a.out[(size_t)(q0 + t) * a.out_stride + head * D + dd] = (bf16)(L > 0.f ? acc / L * kv.v_scale : 0.f);
         } else {
@@ -441,42 +440,40 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     const int lq = lane & 31, lh = lane >> 5;
     const int r = r0 + wave * 32 + lq;
     const bool valid = r < R;
-    const int rc = valid ? r : R - 1, token = rc / G, head = kvh * G + rc - token * G, qpos = before + token;
+    const int rc = valid ? r : R - 1, token = w.by_group.divide(rc), head = kvh * G + rc - token * G, qpos = before + token;
     const int wr = r0 + wave * 32 < R - 1 ? r0 + wave * 32 : R - 1, wl = r0 + wave * 32 + 31 < R - 1 ? r0 + wave * 32 + 31 : R - 1;
     const int wave_min_pos = before + wr / G, wave_max_pos = before + wl / G;
 
-    // A tile's two blocks: their page, 0 in place of one that is not there.
-    struct Tile {
-        int id[2];
-        bool there[2];
-    };
+    // the pages of a tile's two blocks, -1 for one that is not there
     auto look_up = [&](int tile) {
-        Tile t;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int pos = tile * 64 + 32 * b;
-            t.id[b] = pos < hi ? page_of(kv, row, pos) : -1;
-            t.there[b] = t.id[b] >= 0;
-            if (!t.there[b]) t.id[b] = 0;
-        }
+        int2 t;
+        t.x = page_of(kv, row, tile * 64);                   // a tile begins before the end
+        t.y = tile * 64 + 32 < hi ? page_of(kv, row, tile * 64 + 32) : -1;
         return t;
     };
     // this wave's block of a tile: waves 0 and 1 move the first, 2 and 3 the second
     const int wblk = wave >> 1;
-    auto source = [&](const Tile& t, int tile) { return block_base(kv, wblk ? t.id[1] : t.id[0], kvh, tile * 64 + 32 * wblk); };
+    // DMA loads through buffer resources of the wave's half of a K and of a V block: a base in scalar registers, one vector register
+    // for all addresses
+    auto source = [&](int2 t, int tile) {
+        const int id = wblk ? t.y : t.x;                     // page 0 in place of none: read in bounds, masked
+        return block_base(kv, id < 0 ? 0 : id, kvh, tile * 64 + 32 * wblk) + (wave & 1) * (BLK / 2);
+    };
+    const int lane16 = lane * 16;
     auto issue_one = [&](size_t src, int stage, int q) {
-        bf16* st = smem + stage * STAGE;
-        const int piece = wave * NL + q % NL;                // 512 elements each
-        const size_t at = src + (size_t)(piece % (BLK / 512)) * 512 + lane * 8;
-        if (q < NL) __builtin_amdgcn_global_load_lds((gptr_t)(static_cast<const bf16*>(kv.k) + at), (lptr_t)(st + piece * 512), 16, 0, 0);
-        else __builtin_amdgcn_global_load_lds((gptr_t)(static_cast<const bf16*>(kv.v) + at), (lptr_t)(st + 2 * BLK + piece * 512), 16, 0, 0);
+        const int j = q % NL;                                // of the wave's 1 KiB pieces
+        bf16* to = smem + stage * STAGE + (q < NL ? 0 : 2 * BLK) + wave * (BLK / 2) + j * 512;
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc(static_cast<bf16*>(q < NL ? kv.k : kv.v) + src, 0, BLK, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lptr_t)to, 16, lane16, j * 1024, 0, 0);
     };
     u32x4 kreg[NC], vreg[NC];
-    auto fetch = [&](const Tile& t, int tile) {              // e4m3
+    auto fetch = [&](int2 t, int tile) {                     // e4m3
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + 256 * i, blk = NC == 2 ? i : wblk, in = c - blk * (2 * D);
-            const size_t at = block_base(kv, blk ? t.id[1] : t.id[0], kvh, tile * 64 + 32 * blk) + in * 16;
+            const int id = blk ? t.y : t.x;
+            const size_t at = block_base(kv, id < 0 ? 0 : id, kvh, tile * 64 + 32 * blk) + in * 16;
             kreg[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.k) + at);
             vreg[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.v) + at);
         }
@@ -495,7 +492,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         }
     };
 
-    Tile now = look_up(keys.t0), next = now;
+    int2 now = look_up(keys.t0), next = now;
     if (E4M3) {
         fetch(now, keys.t0);
         unpack(0);
@@ -526,24 +523,27 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         __syncthreads();                                     // everyone's; the other stage is free
         const bf16* Ks = smem + stage * STAGE;
         const bf16* Vs = Ks + 2 * BLK;
-        const Tile cur = now;
+        const int2 cur = now;
+        const bool whole = cur.x >= 0 && cur.y >= 0;
         // after the last tile it is requested once more into the idle stage: no branch between the products
         const int nt = tile + 1 < keys.t1 ? tile + 1 : tile;
         now = tile + 1 < keys.t1 ? next : now;
         if (tile + 2 < keys.t1) next = look_up(tile + 2);
         const size_t src = source(now, nt);
         if (E4M3) fetch(now, nt);
-        if (kbase + 64 > hi || kbase < lo || !cur.there[0] || !cur.there[1]) {     // workgroup-uniform
+        if (kbase + 64 > hi || kbase < lo || !whole) {     // workgroup-uniform
             // values that nobody may see: one thread per 8 positions of a head dim
             bf16* vw = smem + stage * STAGE + 2 * BLK;
-            for (int c = tid; c < 8 * D; c += 256) {
+            int c = tid;
+            asm volatile("" : "+v"(c));                      // rare: nothing of this is worth a register over the whole loop
+            for (; c < 8 * D; c += 256) {
                 const int blk = c / (4 * D), piece = (c / D) & 3;
                 const int p = kbase + 32 * blk + 16 * (piece >> 1) + 4 * (piece & 1);
                 bf16x8 v = *reinterpret_cast<bf16x8*>(vw + c * 8);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int pos = p + (e & 3) + 8 * (e >> 2);
-                    if (!(blk ? cur.there[1] : cur.there[0]) || pos < lo || pos >= hi) v[e] = (bf16)0.f;
+                    if ((blk ? cur.y : cur.x) < 0 || pos < lo || pos >= hi) v[e] = (bf16)0.f;
                 }
                 *reinterpret_cast<bf16x8*>(vw + c * 8) = v;
             }
@@ -551,87 +551,82 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
         }
-        // nothing for this wave: behind its rows, or before their windows
-        if (kbase > wave_max_pos || (a.window && kbase + 63 <= wave_min_pos - a.window)) {
-            if (!E4M3)
+        // a wave whose rows see nothing of this tile computes it like the others: as a branch it cost a copy of the accumulators
+        f32x16 sacc[2];
+        // operand fetch runs ahead of the products by hand: each K fragment of the first key block is replaced by the second
+        // block's when its product has gone, and under the second block's the first V fragments are requested
+        constexpr int EVERY = (2 * KS) / (2 * NL);
+        auto k_frag = [&](int kb, int ks) { return *reinterpret_cast<const bf16x8*>(&Ks[kb * BLK + ((ks * 2 + lh) * 32 + lq) * 8]); };
+        auto v_frag = [&](int t, int b) {
+            return *reinterpret_cast<const bf16x8*>(&Vs[(t >> 1) * BLK + ((2 * (t & 1) + lh) * D + b * 32 + lq) * 8]);
+        };
+        bf16x8 ka[KS], vfr[2][DB];
 #pragma unroll
-                for (int q = 0; q < 2 * NL; ++q) issue_one(src, stage ^ 1, q);
-        } else {
-            f32x16 sacc[2];
-            // operand fetch runs ahead of the products by hand: each K fragment of the first key block is replaced by the second
-            // block's when its product has gone, and under the second block's the first V fragments are requested
-            constexpr int EVERY = (2 * KS) / (2 * NL);
-            auto k_frag = [&](int kb, int ks) { return *reinterpret_cast<const bf16x8*>(&Ks[kb * BLK + ((ks * 2 + lh) * 32 + lq) * 8]); };
-            auto v_frag = [&](int t, int b) {
-                return *reinterpret_cast<const bf16x8*>(&Vs[(t >> 1) * BLK + ((2 * (t & 1) + lh) * D + b * 32 + lq) * 8]);
-            };
-            bf16x8 ka[KS], vfr[2][DB];
+        for (int ks = 0; ks < KS; ++ks) ka[ks] = k_frag(0, ks);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) ka[ks] = k_frag(0, ks);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int x = 0; x < 16; ++x) sacc[kb][x] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) sacc[kb][x] = 0.f;
-            __builtin_amdgcn_sched_barrier(0);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], sacc[kb], 0, 0, 0);
-                    if (kb == 0) ka[ks] = k_frag(1, ks);
-                    else if (ks < 2 * DB) vfr[ks / DB][ks % DB] = v_frag(ks / DB, ks % DB);
-                    const int step = kb * KS + ks;
-                    if (!E4M3 && step % EVERY == EVERY - 1) issue_one(src, stage ^ 1, step / EVERY);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            if (kbase + 63 > wave_min_pos || (a.window && kbase <= wave_max_pos - a.window) || !cur.there[0] || !cur.there[1]) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const int pos = kbase + kb * 32 + 8 * (x >> 2) + 4 * lh + (x & 3);
-                        const bool seen = cur.there[kb] && pos <= qpos && (!a.window || pos > qpos - a.window);
-                        sacc[kb][x] = seen ? sacc[kb][x] : -INFINITY;
-                    }
+            for (int ks = 0; ks < KS; ++ks) {
+                sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], sacc[kb], 0, 0, 0);
+                if (kb == 0) ka[ks] = k_frag(1, ks);
+                else if (ks < 2 * DB) vfr[ks / DB][ks % DB] = v_frag(ks / DB, ks % DB);
+                const int step = kb * KS + ks;
+                if (!E4M3 && step % EVERY == EVERY - 1) issue_one(src, stage ^ 1, step / EVERY);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sacc[kb][x]);
-            mx = fmaxf(m, mx * a.scale_log2);                // scale > 0
-            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-            const float ref = finite_or_0(mx);
-            if (__builtin_amdgcn_ballot_w64(mx != m) != 0) { // some row's maximum moved
-                const float alpha = exp2_flush(m - ref);
-                l *= alpha;
-#pragma unroll
-                for (int b = 0; b < DB; ++b)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[b][x] *= alpha;
-                m = mx;
-            }
-            float rs = 0.f;
+        if (kbase + 63 > wave_min_pos || (a.window && kbase <= wave_max_pos - a.window) || !whole) {
+            const int from = first_seen(qpos, a.window);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
-                    const float p = exp2_flush(fmaf(sacc[kb][x], a.scale_log2, -ref));
-                    sacc[kb][x] = p;
-                    rs += p;
+                    const int pos = kbase + kb * 32 + 8 * (x >> 2) + 4 * lh + (x & 3);
+                    const uint32_t reach = (kb ? cur.y : cur.x) >= 0 ? qpos - from + 1 : 0;
+                    sacc[kb][x] = (uint32_t)(pos - from) < reach ? sacc[kb][x] : -INFINITY;
                 }
-            rs += __shfl_xor(rs, 32, kWave);
-            l += rs;
+        }
+        float mx = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                bf16x8 pf;
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[e] = (bf16)sacc[t >> 1][8 * (t & 1) + e];
+            for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sacc[kb][x]);
+        mx = fmaxf(m, mx * a.scale_log2);                // scale > 0
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        const float ref = finite_or_0(mx);
+        if (__builtin_amdgcn_ballot_w64(mx != m) != 0) { // some row's maximum moved
+            const float alpha = exp2_flush(m - ref);
+            l *= alpha;
 #pragma unroll
-                for (int b = 0; b < DB; ++b) {
-                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[t & 1][b], pf, o[b], 0, 0, 0);
-                    if (t + 2 < 4) vfr[t & 1][b] = v_frag(t + 2, b);
-                }
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[b][x] *= alpha;
+            m = mx;
+        }
+        float rs = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const float p = exp2_flush(fmaf(sacc[kb][x], a.scale_log2, -ref));
+                sacc[kb][x] = p;
+                rs += p;
+            }
+        rs += __shfl_xor(rs, 32, kWave);
+        l += rs;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            bf16x8 pf;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pf[e] = (bf16)sacc[t >> 1][8 * (t & 1) + e];
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[t & 1][b], pf, o[b], 0, 0, 0);
+                if (t + 2 < 4) vfr[t & 1][b] = v_frag(t + 2, b);
             }
         }
         if (E4M3) unpack(stage ^ 1);
@@ -650,7 +645,10 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         if (lh == 0) *reinterpret_cast<float2*>(base + kWideRows * D + (wave * 32 + lq) * 2) = make_float2(m, l);
     } else if (valid) {
         const float inv = l > 0.f ? kv.v_scale / l : 0.f;
-        bf16* op = a.out + (size_t)(q0 + token) * a.out_stride + head * D;
+        int at = rc;
+        asm volatile("" : "+v"(at));                         // found again rather than kept over the loop
+        const int tok = w.by_group.divide(at), hd = kvh * G + at - tok * G;
+        bf16* op = a.out + (size_t)(q0 + tok) * a.out_stride + hd * D;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll

@@ -92,6 +92,26 @@ struct PagedQuery {
     int Hq, window;
     float scale_log2;          // score scale times log2 e, and times what 1 in the K cache stands for
 };
+// Division of 0 <= n < 2^31 by a number the host knows: with c = ceil(log2 d), mul = ceil(2^(31+c) / d) fits 32 bits,
+// and n * mul / 2^(31+c) exceeds n / d by less than n / 2^(31+c) < 2^-c <= 1 / d: both have the same floor.
+struct Divisor {
+    uint32_t mul;              // 0: division by one
+    int shift, d;
+    __host__ __device__ int divide(int n) const {
+#ifdef __HIP_DEVICE_COMPILE__
+        return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n;
+#else
+        return mul ? (int)(((uint64_t)(uint32_t)n * mul) >> 32 >> shift) : n;
+#endif
+    }
+};
+inline Divisor divisor(int d) {
+    int c = 0;
+    while (((int64_t)1 << c) < d) ++c;
+    if (c == 0) return Divisor{0, 0, 1};
+    return Divisor{(uint32_t)((((uint64_t)1 << (31 + c)) + d - 1) / d), c - 1, d};
+}
+
 // How the attention of a batch is cut, from the host's copy of its lengths.  A sequence's new tokens times the query heads of a
 // kv head are its rows there.  Narrow: single new tokens, and sequences of few rows; a workgroup takes up to kNarrowRows of them
 // over one chunk of kDecodeChunk positions.  Wide: a workgroup takes kWideRows rows over the keys they see, or over one of
@@ -108,6 +128,7 @@ struct PagedWork {
     int narrow_limit;          // most rows of a sequence of several tokens that is narrow
     int wide_units;            // workgroups of wide rows that have work, times kv heads and ranges
     int splits;
+    Divisor by_heads, by_chunks, by_tiles, by_group;   // n_kv_heads * col_tiles, chunks, col_tiles, G
 };
 size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, int Hkv, int d);
 void launch_paged_attention(const PagedQuery& q, const PagedWork& w, bool e4m3, const BatchView& bv, const PagedView& kv,

@@ -99,6 +99,10 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
     }
     w.splits = units ? (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / units, 16), keys / 256)) : 1;
     w.wide_units = (int)std::min<int64_t>(units, 0x7fffffff);
+    w.by_heads = divisor(Hkv * w.col_tiles);
+    w.by_chunks = divisor(std::max(w.chunks, 1));
+    w.by_tiles = divisor(w.col_tiles);
+    w.by_group = divisor(G);
     return w;
 }
 
