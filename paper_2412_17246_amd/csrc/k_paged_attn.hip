@@ -47,6 +47,16 @@ __device__ __forceinline__ void rotate8(const bf16* q, const float* cs, int half
     }
 }
 
+// the larger, or the sum, of a lane's value and that of its partner 32 lanes on: a vector instruction, no trip through LDS
+__device__ __forceinline__ float pair_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_bit_cast(float, r[0]) + __builtin_bit_cast(float, r[1]);
+}
+
 __device__ __forceinline__ int first_seen(int pos, int window) { return window && pos + 1 > window ? pos + 1 - window : 0; }
 
 // Place of a narrow sequence's tokens among the partial results: single tokens first, then `short_tokens` per sequence.
@@ -242,7 +252,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) m = fmaxf(m, sacc[b][r]);
-        m = fmaxf(m, __shfl_xor(m, 32, kWave)) * a.scale_log2;   // scale > 0
+        m = pair_max(m) * a.scale_log2;                      // scale > 0
         const float ref = finite_or_0(m);
         float l = 0.f;
 #pragma unroll
@@ -253,7 +263,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
                 sacc[b][r] = p;
                 l += p;
             }
-        l += __shfl_xor(l, 32, kWave);
+        l = pair_sum(l);
         f32x16 oacc[DB];
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -514,7 +524,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int x = 0; x < 16; ++x) o[b][x] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f;        // of the row; l over this lane's half of the keys
     if (keys.t0 + 1 < keys.t1) next = look_up(keys.t0 + 1);
 
     for (int tile = keys.t0; tile < keys.t1; ++tile) {
@@ -595,8 +605,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sacc[kb][x]);
-        mx = fmaxf(m, mx * a.scale_log2);                // scale > 0
-        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        mx = fmaxf(m, pair_max(mx) * a.scale_log2);      // scale > 0
         const float ref = finite_or_0(mx);
         if (__builtin_amdgcn_ballot_w64(mx != m) != 0) { // some row's maximum moved
             const float alpha = exp2_flush(m - ref);
@@ -616,7 +625,6 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
                 sacc[kb][x] = p;
                 rs += p;
             }
-        rs += __shfl_xor(rs, 32, kWave);
         l += rs;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -632,6 +640,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         if (E4M3) unpack(stage ^ 1);
     }
 
+    l = pair_sum(l);
     __builtin_amdgcn_s_waitcnt(0x0070);                      // no LDS write may be in flight when the workgroup ends
     if (SPLIT) {
         float* base = partial + ((((size_t)unit.item * G + unit.sub) * Hkv + kvh) * w.splits + unit.split) * (kWideRows * (D + 2));
