@@ -48,13 +48,19 @@ __device__ __forceinline__ void rotate8(const bf16* q, const float* cs, int half
 }
 
 // the larger, or the sum, of a lane's value and that of its partner 32 lanes on: a vector instruction, no trip through LDS
+__device__ __forceinline__ float2 pair_of(float x) {
+    const uint32_t b = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const uint32_t lower = r[0], upper = r[1];
+    return make_float2(__uint_as_float(lower), __uint_as_float(upper));
+}
 __device__ __forceinline__ float pair_max(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+    const float2 v = pair_of(x);
+    return fmaxf(v.x, v.y);
 }
 __device__ __forceinline__ float pair_sum(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return __builtin_bit_cast(float, r[0]) + __builtin_bit_cast(float, r[1]);
+    const float2 v = pair_of(x);
+    return v.x + v.y;
 }
 
 __device__ __forceinline__ int first_seen(int pos, int window) { return window && pos + 1 > window ? pos + 1 - window : 0; }
