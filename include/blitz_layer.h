@@ -471,7 +471,7 @@ typedef struct bz_paged_kv {
     void*          k;               /* device, bz_paged_kv_bytes() bytes, 16-byte aligned */
     void*          v;               /* the same */
     const int32_t* page_table;      /* device, [n_rows][pages_per_row] */
-    int32_t        n_pages;
+    int32_t        n_pages;         /* n_pages * n_kv_heads * page_size / 32 < 2^31 */
     int32_t        page_size;       /* a power of two from 32 to 1024 */
     int32_t        n_rows;
     int32_t        pages_per_row;   /* pages_per_row * page_size < 2^31 */

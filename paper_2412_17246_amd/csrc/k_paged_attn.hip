@@ -31,19 +31,20 @@ __device__ __forceinline__ bf16x8 e4m3_to_bf16(uint32_t a, uint32_t b) {
     return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
-// 8 pairs (j0 + e, j0 + e + d/2) of a query, rotated if there is a table, rounded to bf16
-__device__ __forceinline__ void rotate8(const bf16* q, const float* cs, int half, bf16x8& lo8, bf16x8& hi8) {
+// 8 pairs (j0 + e, j0 + e + d/2) of a query: as they are, or rotated, scaled and rounded to bf16 once
+template <bool ROTATE>
+__device__ __forceinline__ void query8(const bf16* q, const float* cs, float scale, int half, bf16x8& lo8, bf16x8& hi8) {
     lo8 = *reinterpret_cast<const bf16x8*>(q);
     hi8 = *reinterpret_cast<const bf16x8*>(q + half);
-    if (!cs) return;
+    if (!ROTATE) return;
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
         const float4 v = *reinterpret_cast<const float4*>(cs + 2 * e);
         const float l0 = (float)lo8[e], h0 = (float)hi8[e], l1 = (float)lo8[e + 1], h1 = (float)hi8[e + 1];
-        lo8[e] = (bf16)(l0 * v.x - h0 * v.y);
-        hi8[e] = (bf16)(h0 * v.x + l0 * v.y);
-        lo8[e + 1] = (bf16)(l1 * v.z - h1 * v.w);
-        hi8[e + 1] = (bf16)(h1 * v.z + l1 * v.w);
+        lo8[e] = (bf16)((l0 * v.x - h0 * v.y) * scale);
+        hi8[e] = (bf16)((h0 * v.x + l0 * v.y) * scale);
+        lo8[e + 1] = (bf16)((l1 * v.z - h1 * v.w) * scale);
+        hi8[e + 1] = (bf16)((h1 * v.z + l1 * v.w) * scale);
     }
 }
 
@@ -62,6 +63,61 @@ __device__ __forceinline__ float pair_sum(float x) {
     const float2 v = pair_of(x);
     return v.x + v.y;
 }
+
+// The softmax of a tile of 64 keys for rows that lane pairs own, against a reference that only has to be within 2^kLag of the
+// largest score so far: then most tiles leave the accumulators alone.  Weights are at most 2^kLag, and the row's largest at
+// least 1 when the reference was set; everything is relative to it and no bits are lost.
+constexpr float kLag = 8.f;
+template <int DB, bool SCALED>
+struct RowSoftmax {
+    float ref = 0.f, l = 0.f;            // l over this lane's half of the keys
+    bool seen = false;                   // the reference is one
+    f32x16 start;                        // SCALED: -ref sixteen times, what the score products start from
+
+    __device__ __forceinline__ void init() {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) start[x] = 0.f;
+    }
+    // scores (SCALED: in base 2, the reference taken off by the product; else raw) to weights in bf16
+    __device__ __forceinline__ void weigh(f32x16 (&s)[2], float scale, f32x16 (&o)[DB], bf16x8 (&pf)[4]) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[kb][x]);
+        mx = SCALED ? pair_max(mx) : fmaf(pair_max(mx), scale, -ref);      // above the reference
+        const bool move = mx > (seen ? kLag : -INFINITY);
+        if (__builtin_amdgcn_ballot_w64(move) != 0) {
+            const float up = move ? mx : 0.f, alpha = move && !seen ? 0.f : exp2_flush(-up);
+            seen |= move;
+            ref += up;
+            l *= alpha;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[b][x] *= alpha;
+            if (SCALED) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[kb][x] -= up;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) start[x] = -ref;
+            }
+        }
+        const bf16x2 ones = {(bf16)1.f, (bf16)1.f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float a = s[t >> 1][8 * (t & 1) + e], b = s[t >> 1][8 * (t & 1) + e + 1];
+                const bf16x2 p = {(bf16)exp2_flush(SCALED ? a : fmaf(a, scale, -ref)), (bf16)exp2_flush(SCALED ? b : fmaf(b, scale, -ref))};
+                l = __builtin_amdgcn_fdot2_f32_bf16(p, ones, l, false);    // the sum of the weights as the product will use them
+                pf[t][e] = p[0];
+                pf[t][e + 1] = p[1];
+            }
+    }
+};
 
 __device__ __forceinline__ int first_seen(int pos, int window) { return window && pos + 1 > window ? pos + 1 - window : 0; }
 
@@ -396,8 +452,8 @@ struct WideUnit {
 };
 // XCD-aware: workgroups go to the eight XCDs in turn; with a multiple of eight kv heads each XCD takes whole kv heads and walks
 // one after the other, longest key ranges first, so that what runs on it at a time shares the K and V in its L2.
-__device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int G, int Hkv, int splits) {
-    const int per_head = n_items * G * splits;
+__device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int subs, int Hkv, int splits) {
+    const int per_head = n_items * subs * splits;
     WideUnit u;
     int rest;
     if ((Hkv & 7) == 0) {
@@ -408,19 +464,19 @@ __device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int G, int Hkv
         u.kvh = b / per_head;
         rest = b - u.kvh * per_head;
     }
-    u.item = rest / (G * splits);
-    rest -= u.item * (G * splits);
-    u.sub = G - 1 - rest / splits;
+    u.item = rest / (subs * splits);
+    rest -= u.item * (subs * splits);
+    u.sub = subs - 1 - rest / splits;
     u.split = rest % splits;
     return u;
 }
 
-// the tiles of 64 keys that rows r0 .. r0 + 127 see, or the range of them that `split` names
+// the tiles of 64 keys that `rows` rows from r0 on see, or the range of them that `split` names
 struct WideKeys {
     int t0, t1, splits;
 };
-__device__ __forceinline__ WideKeys wide_keys(int before, int r0, int R, int G, int window, int split, int splits) {
-    const int first = before + r0 / G, last = before + (r0 + kWideRows < R ? r0 + kWideRows - 1 : R - 1) / G;
+__device__ __forceinline__ WideKeys wide_keys(int before, int r0, int rows, int R, int G, int window, int split, int splits) {
+    const int first = before + r0 / G, last = before + (r0 + rows < R ? r0 + rows - 1 : R - 1) / G;
     WideKeys k;
     k.t0 = first_seen(first, window) >> 6;
     k.t1 = (last >> 6) + 1;
@@ -431,7 +487,31 @@ __device__ __forceinline__ WideKeys wide_keys(int before, int r0, int R, int G, 
     return k;
 }
 
-template <int D, bool E4M3, bool SPLIT>
+// Where the two blocks of a tile of 64 keys lie, counted in blocks of 32 positions from the start of the cache, -1 for one that is
+// behind the sequence or on a page that is not there.  A wave keeps 64 tiles' in its lanes: the table is read once per 4096
+// positions, and a tile's entry costs a lane read, where a scalar load behind LDS reads would wait for all of them.
+struct TileMap {
+    int base, x, y;
+    __device__ __forceinline__ void load(const PagedView& kv, int row, int kvh, int hi, int from) {
+        base = from;
+        const int pos = (int)(((uint32_t)from + (threadIdx.x & 63)) * 64), per_page = kv.page_shift - 5;
+        auto block = [&](int p) {
+            const int id = p < hi && p >= 0 ? page_of(kv, row, p) : -1;
+            return id < 0 ? -1 : ((id * kv.Hkv + kvh) << per_page) + ((p >> 5) & ((1 << per_page) - 1));
+        };
+        x = block(pos);
+        y = block(pos + 32);
+    }
+    __device__ __forceinline__ int2 operator()(const PagedView& kv, int row, int kvh, int hi, int tile) {
+        if (tile >= base + 64) load(kv, row, kvh, hi, tile);
+        return make_int2(__builtin_amdgcn_readlane(x, tile - base), __builtin_amdgcn_readlane(y, tile - base));
+    }
+};
+// first element of a block; the cache's first block in place of none: read in bounds, masked
+template <int D>
+__device__ __forceinline__ size_t block_start(int block) { return (size_t)(uint32_t)(block < 0 ? 0 : block) * (32 * D); }
+
+template <int D, bool E4M3, bool ROTATE, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
                                                             float* __restrict__ partial) {
     constexpr int DB = D / 32, KS = D / 16, BLK = 32 * D;
@@ -447,7 +527,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s], row = bv.seq_slot[s];
     const int R = n * G, r0 = (qt * G + unit.sub) * kWideRows;
     if (r0 >= R || R <= w.narrow_limit) return;
-    const WideKeys keys = wide_keys(before, r0, R, G, a.window, unit.split, w.splits);
+    const WideKeys keys = wide_keys(before, r0, kWideRows, R, G, a.window, unit.split, w.splits);
     if (SPLIT && keys.t0 >= keys.t1) return;
     const int hi = before + n, lo = first_seen(before + r0 / G, a.window);
     const int kvh = unit.kvh;
@@ -460,21 +540,14 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     const int wr = r0 + wave * 32 < R - 1 ? r0 + wave * 32 : R - 1, wl = r0 + wave * 32 + 31 < R - 1 ? r0 + wave * 32 + 31 : R - 1;
     const int wave_min_pos = before + wr / G, wave_max_pos = before + wl / G;
 
-    // the pages of a tile's two blocks, -1 for one that is not there
-    auto look_up = [&](int tile) {
-        int2 t;
-        t.x = page_of(kv, row, tile * 64);                   // a tile begins before the end
-        t.y = tile * 64 + 32 < hi ? page_of(kv, row, tile * 64 + 32) : -1;
-        return t;
-    };
+    TileMap map;
+    map.load(kv, row, kvh, hi, keys.t0);
+    auto look_up = [&](int tile) { return map(kv, row, kvh, hi, tile); };
     // this wave's block of a tile: waves 0 and 1 move the first, 2 and 3 the second
     const int wblk = wave >> 1;
     // DMA loads through buffer resources of the wave's half of a K and of a V block: a base in scalar registers, one vector register
     // for all addresses
-    auto source = [&](int2 t, int tile) {
-        const int id = wblk ? t.y : t.x;                     // page 0 in place of none: read in bounds, masked
-        return block_base(kv, id < 0 ? 0 : id, kvh, tile * 64 + 32 * wblk) + (wave & 1) * (BLK / 2);
-    };
+    auto source = [&](int2 t) { return block_start<D>(wblk ? t.y : t.x) + (wave & 1) * (BLK / 2); };
     const int lane16 = lane * 16;
     auto issue_one = [&](size_t src, int stage, int q) {
         const int j = q % NL;                                // of the wave's 1 KiB pieces
@@ -484,12 +557,11 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lptr_t)to, 16, lane16, j * 1024, 0, 0);
     };
     u32x4 kreg[NC], vreg[NC];
-    auto fetch = [&](int2 t, int tile) {                     // e4m3
+    auto fetch = [&](int2 t) {                               // e4m3
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + 256 * i, blk = NC == 2 ? i : wblk, in = c - blk * (2 * D);
-            const int id = blk ? t.y : t.x;
-            const size_t at = block_base(kv, id < 0 ? 0 : id, kvh, tile * 64 + 32 * blk) + in * 16;
+            const size_t at = block_start<D>(blk ? t.y : t.x) + in * 16;
             kreg[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.k) + at);
             vreg[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(kv.v) + at);
         }
@@ -508,12 +580,12 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         }
     };
 
-    int2 now = look_up(keys.t0), next = now;
+    int2 now = look_up(keys.t0);
     if (E4M3) {
-        fetch(now, keys.t0);
+        fetch(now);
         unpack(0);
     } else {
-        const size_t src = source(now, keys.t0);
+        const size_t src = source(now);
 #pragma unroll
         for (int q = 0; q < 2 * NL; ++q) issue_one(src, 0, q);
     }
@@ -521,17 +593,18 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     bf16x8 qf[KS];
     {
         const bf16* qp = a.q + (size_t)(q0 + token) * a.q_stride + head * D;
-        const float* cs = a.rope.tab ? rope_row(a.rope, qpos, D) : nullptr;
+        const float* cs = ROTATE ? rope_row(a.rope, qpos, D) : nullptr;
 #pragma unroll
-        for (int ks = 0; ks < KS / 2; ++ks) rotate8(qp + ks * 16 + lh * 8, cs ? cs + 2 * (ks * 16 + lh * 8) : nullptr, D / 2, qf[ks], qf[ks + KS / 2]);
+        for (int ks = 0; ks < KS / 2; ++ks)
+            query8<ROTATE>(qp + ks * 16 + lh * 8, cs + 2 * (ks * 16 + lh * 8), a.scale_log2, D / 2, qf[ks], qf[ks + KS / 2]);
     }
     f32x16 o[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int x = 0; x < 16; ++x) o[b][x] = 0.f;
-    float m = -INFINITY, l = 0.f;        // of the row; l over this lane's half of the keys
-    if (keys.t0 + 1 < keys.t1) next = look_up(keys.t0 + 1);
+    RowSoftmax<DB, ROTATE> rows;         // queries that were rotated are scaled as well
+    rows.init();
 
     for (int tile = keys.t0; tile < keys.t1; ++tile) {
         const int stage = (tile - keys.t0) & 1, kbase = tile * 64;
@@ -542,11 +615,9 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         const int2 cur = now;
         const bool whole = cur.x >= 0 && cur.y >= 0;
         // after the last tile it is requested once more into the idle stage: no branch between the products
-        const int nt = tile + 1 < keys.t1 ? tile + 1 : tile;
-        now = tile + 1 < keys.t1 ? next : now;
-        if (tile + 2 < keys.t1) next = look_up(tile + 2);
-        const size_t src = source(now, nt);
-        if (E4M3) fetch(now, nt);
+        if (tile + 1 < keys.t1) now = look_up(tile + 1);
+        const size_t src = source(now);
+        if (E4M3) fetch(now);
         if (kbase + 64 > hi || kbase < lo || !whole) {     // workgroup-uniform
             // values that nobody may see: one thread per 8 positions of a head dim
             bf16* vw = smem + stage * STAGE + 2 * BLK;
@@ -579,16 +650,13 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         bf16x8 ka[KS], vfr[2][DB];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) ka[ks] = k_frag(0, ks);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) sacc[kb][x] = 0.f;
+        if (!ROTATE) rows.init();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], sacc[kb], 0, 0, 0);
+                sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], ks ? sacc[kb] : rows.start, 0, 0, 0);
                 if (kb == 0) ka[ks] = k_frag(1, ks);
                 else if (ks < 2 * DB) vfr[ks / DB][ks % DB] = v_frag(ks / DB, ks % DB);
                 const int step = kb * KS + ks;
@@ -606,47 +674,20 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
                     sacc[kb][x] = (uint32_t)(pos - from) < reach ? sacc[kb][x] : -INFINITY;
                 }
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sacc[kb][x]);
-        mx = fmaxf(m, pair_max(mx) * a.scale_log2);      // scale > 0
-        const float ref = finite_or_0(mx);
-        if (__builtin_amdgcn_ballot_w64(mx != m) != 0) { // some row's maximum moved
-            const float alpha = exp2_flush(m - ref);
-            l *= alpha;
-#pragma unroll
-            for (int b = 0; b < DB; ++b)
-#pragma unroll
-                for (int x = 0; x < 16; ++x) o[b][x] *= alpha;
-            m = mx;
-        }
-        float rs = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const float p = exp2_flush(fmaf(sacc[kb][x], a.scale_log2, -ref));
-                sacc[kb][x] = p;
-                rs += p;
-            }
-        l += rs;
+        bf16x8 pf[4];
+        rows.weigh(sacc, a.scale_log2, o, pf);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            bf16x8 pf;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) pf[e] = (bf16)sacc[t >> 1][8 * (t & 1) + e];
 #pragma unroll
             for (int b = 0; b < DB; ++b) {
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[t & 1][b], pf, o[b], 0, 0, 0);
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[t & 1][b], pf[t], o[b], 0, 0, 0);
                 if (t + 2 < 4) vfr[t & 1][b] = v_frag(t + 2, b);
             }
         }
         if (E4M3) unpack(stage ^ 1);
     }
 
-    l = pair_sum(l);
+    const float l = pair_sum(rows.l);
     __builtin_amdgcn_s_waitcnt(0x0070);                      // no LDS write may be in flight when the workgroup ends
     if (SPLIT) {
         float* base = partial + ((((size_t)unit.item * G + unit.sub) * Hkv + kvh) * w.splits + unit.split) * (kWideRows * (D + 2));
@@ -657,7 +698,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
             for (int r4 = 0; r4 < 4; ++r4)
                 *reinterpret_cast<float4*>(op + ((b * 4 + r4) * 2 + lh) * 128) =
                     make_float4(o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]);
-        if (lh == 0) *reinterpret_cast<float2*>(base + kWideRows * D + (wave * 32 + lq) * 2) = make_float2(m, l);
+        if (lh == 0) *reinterpret_cast<float2*>(base + kWideRows * D + (wave * 32 + lq) * 2) = make_float2(rows.seen ? rows.ref : -INFINITY, l);
     } else if (valid) {
         const float inv = l > 0.f ? kv.v_scale / l : 0.f;
         int at = rc;
@@ -688,7 +729,7 @@ __global__ __launch_bounds__(256) void paged_wide_join_kernel(PagedQuery a, Page
     const int R = n * G, r0 = (qt * G + sub) * kWideRows;
     const int x = part * 32 + (threadIdx.x & 31), r = r0 + x;
     if (r >= R || R <= w.narrow_limit) return;
-    const WideKeys keys = wide_keys(before, r0, R, G, a.window, 0, w.splits);
+    const WideKeys keys = wide_keys(before, r0, kWideRows, R, G, a.window, 0, w.splits);
     const float* base = partial + (((size_t)item * G + sub) * Hkv + kvh) * w.splits * (kWideRows * (D + 2));
     constexpr size_t UNIT = kWideRows * (D + 2);
     float M = -INFINITY;
@@ -733,12 +774,12 @@ size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, in
     return narrow_bytes(w, bv, Hq, d) + wide;
 }
 
-template <int D, bool E4M3, bool SPLIT>
+template <int D, bool E4M3, bool ROTATE, bool SPLIT>
 static void launch_wide(const PagedQuery& q, const PagedWork& w, const BatchView& bv, const PagedView& kv, float* ws, hipStream_t st) {
     constexpr int kLds = 2 * 4 * 32 * D * (int)sizeof(bf16);             // two stages of a K and a V tile
     static LdsLimit limit;
-    (void)limit.raise(reinterpret_cast<const void*>(paged_wide_kernel<D, E4M3, SPLIT>), kLds);
-    hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, SPLIT>), dim3((unsigned)(bv.n_prefill_items * q.Hq * w.splits)), dim3(256), kLds, st, q,
+    (void)limit.raise(reinterpret_cast<const void*>(paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), kLds);
+    hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), dim3((unsigned)(bv.n_prefill_items * q.Hq * w.splits)), dim3(256), kLds, st, q,
                        w, bv, kv, ws);
     if (SPLIT) hipLaunchKernelGGL(paged_wide_join_kernel<D>, dim3((unsigned)(bv.n_prefill_items * q.Hq * 4)), dim3(256), 0, st, q, w, bv, kv, ws);
 }
@@ -758,7 +799,9 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
     }
     if (w.wide_units > 0) {
         float* wide = ws ? ws + narrow_bytes(w, bv, q.Hq, D) / sizeof(float) : nullptr;
-        (w.splits > 1 ? launch_wide<D, E4M3, true> : launch_wide<D, E4M3, false>)(q, w, bv, kv, wide, st);
+        auto rows = q.rope.tab ? (w.splits > 1 ? launch_wide<D, E4M3, true, true> : launch_wide<D, E4M3, true, false>)
+                               : (w.splits > 1 ? launch_wide<D, E4M3, false, true> : launch_wide<D, E4M3, false, false>);
+        rows(q, w, bv, kv, wide, st);
     }
 }
 
