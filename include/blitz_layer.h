@@ -511,6 +511,9 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  * Results depend within rounding on the other sequences of the batch, whose lengths say how key ranges are cut; the same call
  * gives the same bits every time.
  *
+ * The stream of an append or an attention has to exist until the batch is next rebuilt, advanced or destroyed: that is when the
+ * library orders a change behind what was enqueued there.
+ *
  * Both operations may be captured into a graph.  It replays the batch as it was: rebuilding, advancing or destroying the batch
  * means capturing again, and is not ordered behind replays by the library.  Under capture a batch that was last rebuilt or
  * advanced on another stream is refused (BZ_ESTATE). */

@@ -683,15 +683,16 @@ class PagedKv:
         if self.lib.bz_paged_kv_bytes(C.byref(self.desc)) != k.numel() * k.element_size():
             raise BzError(-1, "bz_paged_kv")
         self._ref = C.byref(self.desc)
-        self._act = act
+        self._act, self._device = act, k.device
 
 
 def _rows(kv: PagedKv, batch: Batch, x, what: str) -> int:
     """Checks the packed rows of a batch's heads and returns how many elements a row has."""
-    if x.dim() != 2 or x.shape[0] < batch.T or x.stride(1) != 1 or x.dtype != kv._act or x.device != kv.k.device:
-        raise ValueError(f"{what} must be [{batch.T} rows or more, heads * head_dim] of {kv._act} on {kv.k.device}, "
+    shape = x.shape
+    if len(shape) != 2 or shape[0] < batch.T or x.stride(1) != 1 or x.dtype != kv._act or x.device != kv._device:
+        raise ValueError(f"{what} must be [{batch.T} rows or more, heads * head_dim] of {kv._act} on {kv._device}, "
                          "the elements of a row side by side")
-    return x.shape[1]
+    return shape[1]
 
 
 def _pitch(x) -> int:
@@ -702,7 +703,7 @@ def _pitch(x) -> int:
 def _rope(kv: PagedKv, rope):
     if rope is None:
         return 0, 0
-    if rope.shape[1:] != (kv.head_dim // 2, 2) or not rope.is_contiguous() or rope.element_size() != 4 or rope.device != kv.k.device:
+    if rope.shape[1:] != (kv.head_dim // 2, 2) or not rope.is_contiguous() or rope.element_size() != 4 or rope.device != kv._device:
         raise ValueError("rope must be a contiguous float32 tensor [positions, head_dim/2, 2] on the cache's device")
     return rope.data_ptr(), rope.shape[0]
 
@@ -744,7 +745,7 @@ def op_paged_read(kv: PagedKv, row: int, pos0: int, n: int, k, v, stream=None) -
     """Positions pos0 .. pos0 + n - 1 of a table row into k and v, contiguous [n, n_kv_heads, head_dim]."""
     need = n * kv.n_kv_heads * kv.head_dim
     for x in (k, v):
-        if x.dtype != kv._act or x.device != kv.k.device or not x.is_contiguous() or x.numel() < need:
+        if x.dtype != kv._act or x.device != kv._device or not x.is_contiguous() or x.numel() < need:
             raise ValueError(f"k and v must be contiguous {kv._act} tensors of [n, n_kv_heads, head_dim] on the cache's device")
     rc = kv.lib.bz_op_paged_read(kv._ref, row, pos0, n, k.data_ptr(), v.data_ptr(), stream.cuda_stream if stream else 0)
     if rc:

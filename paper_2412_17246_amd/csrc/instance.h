@@ -61,7 +61,8 @@ struct bz_batch {
     // Ordering between streams.  A batch may be run by two instances with different compute streams (a split
     // pair).  Runs that must be ordered against a later device-side change of the batch (advance, rebuild)
     // leave an event per stream; the change leaves one that later runs on other streams wait for.
-    struct Use { hipStream_t st; hipEvent_t ev; };
+    // (`unmarked`: the event is behind by single operations, and is recorded when a change asks for it)
+    struct Use { hipStream_t st; hipEvent_t ev; bool unmarked; };
     mutable std::vector<Use> runs;
     hipStream_t changed_on = nullptr;
     hipEvent_t changed_ev = nullptr;
@@ -72,7 +73,7 @@ namespace bz {
 BatchView batch_view(const bz_batch* b);
 // around the kernels that read a batch on stream `st`
 int batch_before_run(const bz_batch* b, hipStream_t st);
-int batch_after_run(const bz_batch* b, hipStream_t st);
+int batch_after_run(const bz_batch* b, hipStream_t st, bool mark);
 int stream_is_capturing(hipStream_t st, bool* out);
 }  // namespace bz
 

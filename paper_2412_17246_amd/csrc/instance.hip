@@ -840,9 +840,15 @@ void bind_batch(bz_batch* b) {
 }
 
 // Orders stream `st` behind every run of the batch that was enqueued on another stream.
-int wait_for_runs_elsewhere(const bz_batch* b, hipStream_t st) {
-    for (const bz_batch::Use& u : b->runs)
-        if (u.st != st) HIP_TRY(hipStreamWaitEvent(st, u.ev, 0));
+int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
+    for (bz_batch::Use& u : b->runs) {
+        if (u.st == st) continue;
+        if (u.unmarked) {
+            HIP_TRY(hipEventRecord(u.ev, u.st));
+            u.unmarked = false;
+        }
+        HIP_TRY(hipStreamWaitEvent(st, u.ev, 0));
+    }
     return BZ_OK;
 }
 
@@ -896,8 +902,9 @@ int batch_before_run(const bz_batch* b, hipStream_t st) {
 }
 
 // A batch that can change on the device later (advance, rebuild), possibly on another stream, gets a marker behind the
-// kernels that read it: one event per stream that ever ran it, re-recorded.
-int batch_after_run(const bz_batch* b, hipStream_t st) {
+// kernels that read it: one event per stream that ever ran it.  bz_run_layers records it again after every run; after a single
+// operation, which takes as little as 3 us, recording would cost another 3 us of the host's time and is left to the change.
+int batch_after_run(const bz_batch* b, hipStream_t st, bool mark) {
     if (!b->all_decode && !b->staging) return BZ_OK;
     bool capturing = false;
     const int rc = stream_is_capturing(st, &capturing);
@@ -909,10 +916,11 @@ int batch_after_run(const bz_batch* b, hipStream_t st) {
     if (!use) {
         hipEvent_t ev = nullptr;
         HIP_TRY(hipEventCreateWithFlags(&ev, hipEventDisableTiming));
-        b->runs.push_back(bz_batch::Use{st, ev});
+        b->runs.push_back(bz_batch::Use{st, ev, false});
         use = &b->runs.back();
     }
-    HIP_TRY(hipEventRecord(use->ev, st));
+    use->unmarked = !mark;
+    if (mark) HIP_TRY(hipEventRecord(use->ev, st));
     return BZ_OK;
 }
 
@@ -937,7 +945,12 @@ int bz_batch_destroy(bz_batch* b) {
         if (b->staged_ev[h]) (void)hipEventDestroy(b->staged_ev[h]);
     }
     if (b->changed_valid) (void)hipEventSynchronize(b->changed_ev);
-    for (const bz_batch::Use& u : b->runs) { (void)hipEventSynchronize(u.ev); (void)hipEventDestroy(u.ev); }
+    for (const bz_batch::Use& u : b->runs) {
+        bool capturing = false;
+        if (u.unmarked && stream_is_capturing(u.st, &capturing) == BZ_OK && !capturing) (void)hipEventRecord(u.ev, u.st);
+        (void)hipEventSynchronize(u.ev);
+        (void)hipEventDestroy(u.ev);
+    }
     if (b->changed_ev) (void)hipEventDestroy(b->changed_ev);
     if (b->own_dev && b->dev) (void)hipFree(b->dev);
     delete b;
@@ -1196,7 +1209,7 @@ int bz_run_layers(bz_instance* I, int a, int b, const bz_batch* batch, void* hid
         HIP_TRY(hipGetLastError());
     }
     {
-        const int rc = batch_after_run(batch, st);
+        const int rc = batch_after_run(batch, st, true);
         if (rc) return rc;
     }
     I->stats.tokens_run += (uint64_t)T * (uint64_t)(b - a);

@@ -110,7 +110,7 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
 int launched(const bz_batch* b, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "launch");
-    return batch_after_run(b, st);
+    return batch_after_run(b, st, false);
 }
 
 }  // namespace
