@@ -130,16 +130,22 @@ __device__ __forceinline__ size_t partial_at(const PagedWork& w, int n_decode, i
 }  // namespace
 
 // ---------------------------------------------------------------------------------------------
-// Narrow: a workgroup reads one chunk of 256 positions of one kv head once, for up to RT rows.  Each of its four waves owns 64
-// positions, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose row
-// operand is the cache as it lies in memory; rows of the problem are the 32 columns.  The four results are merged through LDS in wave
-// order.  Bound by the cache's bytes.
+// Narrow: a workgroup reads one chunk of 256 * STEPS positions of one kv head once, for up to RT rows.  Each of its four waves takes
+// 64 positions at a time, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose
+// row operand is the cache as it lies in memory; rows of the problem are the 32 columns.  The four waves' results are merged through
+// LDS in wave order.  Bound by the cache's bytes.
+//
+// A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d * STEPS cache elements: a sixteenth of the
+// bytes for eight rows of e4m3, an eighth for 32 rows of bf16, at one step.  With two steps half of that; the second step's K is
+// requested when the first step's has been used, its V likewise (AHEAD: both steps before anything, where e4m3 leaves the registers).
 // ---------------------------------------------------------------------------------------------
-template <int D, bool E4M3, int RT, int WAVES>
+template <int D, bool E4M3, int RT, int STEPS, int WAVES>
 __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(256) void paged_narrow_kernel(
     PagedQuery a, PagedWork w, BatchView bv, PagedView kv, float* __restrict__ partial) {
-    constexpr int CH = kDecodeChunk, KS = D / 16, DB = D / 32, LD = D + 8;
+    constexpr int CH = kDecodeChunk * STEPS, KS = D / 16, DB = D / 32, LD = D + 8;
     constexpr int NF = E4M3 ? D / 32 : D / 16;               // 16-byte loads per lane and block, of K and again of V
+    constexpr bool AHEAD = E4M3 && STEPS == 2;
+    constexpr int SETS = AHEAD ? 2 : 1;
     __shared__ float wmx[4][RT], wsum[4][RT];
     __shared__ float osh[4][RT][D];
     __shared__ __attribute__((aligned(16))) bf16 qs[RT][LD];
@@ -150,11 +156,19 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     const int hc = blockIdx.x - e * w.by_heads.d, kvh = w.by_tiles.divide(hc), ct = hc - kvh * w.by_tiles.d;
     int i, s, row, chunk;
     if (e < w.list) {
-        const int4 item = bv.decode_work[2 * e];
-        s = item.x;
-        row = item.y;
-        i = item.z;
-        chunk = e - bv.decode_work[2 * e + 1].x;
+        const int4 of = bv.decode_work[2 * e + 1];
+        if (STEPS == 1) {
+            const int4 item = bv.decode_work[2 * e];
+            s = item.x;
+            row = item.y;
+            i = item.z;
+            chunk = e - of.x;
+        } else {
+            i = of.y;
+            s = bv.decode_seqs[i];
+            row = bv.seq_slot[s];
+            chunk = e - of.z;
+        }
     } else {
         e -= w.list;
         i = w.by_chunks.divide(e);
@@ -172,17 +186,16 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lq = lane & 31, lh = lane >> 5;
-    const int w0 = c0 + wave * 64;
-    const bool live = w0 < hi;                               // wave-uniform
-    int id[2];
-    bool there[2];
+    // positions of a step; wave-uniform
+    auto begin = [&](int step) { return c0 + (step * 4 + wave) * 64; };
+    int id[STEPS][2];                                        // pages, -1 for one that is not there
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int pos = w0 + 32 * b;
-        id[b] = pos < hi ? page_of(kv, row, pos) : -1;
-        there[b] = id[b] >= 0;
-        if (!there[b]) id[b] = 0;                            // read in bounds, masked below
-    }
+    for (int x = 0; x < STEPS; ++x)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int pos = begin(x) + 32 * b;
+            id[x][b] = pos < hi ? page_of(kv, row, pos) : -1;
+        }
 
     // queries: unit = 8 pairs of a row, requested before the stream
     constexpr int UPR = D / 16;
@@ -196,44 +209,53 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     if (a.rope.tab) {
         const float* c = rope_row(a.rope, before + ut, D) + 2 * uj;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) cs[e] = *reinterpret_cast<const f32x4*>(c + 4 * e);
+        for (int x = 0; x < 4; ++x) cs[x] = *reinterpret_cast<const f32x4*>(c + 4 * x);
     }
     __builtin_amdgcn_sched_barrier(0);
 
-    u32x4 kf[2][NF], vf[2][NF];
-    if (live) {
-        // non-temporal: nobody reads them again.  A base in scalar registers, one vector register for all addresses of K, one for V.
-        constexpr int EL = E4M3 ? 1 : 2;
-        auto block = [&](void* cache, int b) {
-            return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(cache) + block_base(kv, id[b], kvh, w0 + 32 * b) * EL, 0,
-                                                     32 * D * EL, 0x00020000);
-        };
-        auto load = [&](__amdgpu_buffer_rsrc_t r, int lane_at, int at) {
-            return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 2));
-        };
-        // pieces of K: [piece][position]; a step takes two, one per lane half.  Pieces of V: [2t + h][j], or [h][j] with both t.
-        const int lane_k = (lh * 32 + lq) * 16, lane_v = (lh * D + lq) * 16;
+    // non-temporal: nobody reads them again.  A base in scalar registers, one vector register for all addresses of K, one for V.
+    constexpr int EL = E4M3 ? 1 : 2;
+    auto block = [&](void* cache, int step, int b) {
+        const int page = id[step][b] < 0 ? 0 : id[step][b];  // read in bounds, masked below
+        return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(cache) + block_base(kv, page, kvh, begin(step) + 32 * b) * EL, 0,
+                                                 32 * D * EL, 0x00020000);
+    };
+    auto load = [&](__amdgpu_buffer_rsrc_t r, int lane_at, int at) {
+        return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 2));
+    };
+    // pieces of K: [piece][position]; a step takes two, one per lane half.  Pieces of V: [2t + h][j], or [h][j] with both t.
+    const int lane_k = (lh * 32 + lq) * 16, lane_v = (lh * D + lq) * 16;
+    u32x4 kf[SETS][2][NF], vf[SETS][2][NF];
+    auto load_k = [&](int step) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const __amdgpu_buffer_rsrc_t r = block(kv.k, b);
+            const __amdgpu_buffer_rsrc_t r = block(kv.k, step, b);
 #pragma unroll
-            for (int x = 0; x < NF; ++x) kf[b][x] = load(r, lane_k, x * 1024);
+            for (int x = 0; x < NF; ++x) kf[AHEAD ? step : 0][b][x] = load(r, lane_k, x * 1024);
         }
+    };
+    auto load_v = [&](int step) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const __amdgpu_buffer_rsrc_t r = block(kv.v, b);
+            const __amdgpu_buffer_rsrc_t r = block(kv.v, step, b);
 #pragma unroll
-            for (int x = 0; x < NF; ++x) vf[b][x] = load(r, lane_v, E4M3 ? x * 512 : (x / DB) * (2 * D * 16) + (x % DB) * 512);
+            for (int x = 0; x < NF; ++x) vf[AHEAD ? step : 0][b][x] = load(r, lane_v, E4M3 ? x * 512 : (x / DB) * (2 * D * 16) + (x % DB) * 512);
         }
-    }
+    };
+#pragma unroll
+    for (int x = 0; x < SETS; ++x)
+        if (begin(x) < hi) {
+            load_k(x);
+            load_v(x);
+        }
     __builtin_amdgcn_sched_barrier(0);
     if (a.rope.tab) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float c = cs[e >> 1][2 * (e & 1)], sn = cs[e >> 1][2 * (e & 1) + 1];
-            const float x = (float)qlo[e], y = (float)qhi[e];
-            qlo[e] = (bf16)(x * c - y * sn);
-            qhi[e] = (bf16)(y * c + x * sn);
+        for (int x = 0; x < 8; ++x) {
+            const float c = cs[x >> 1][2 * (x & 1)], sn = cs[x >> 1][2 * (x & 1) + 1];
+            const float y = (float)qlo[x], z = (float)qhi[x];
+            qlo[x] = (bf16)(y * c - z * sn);
+            qhi[x] = (bf16)(z * c + y * sn);
         }
     }
     if (tid < units) {
@@ -245,107 +267,123 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 
-    if (live) {
-        const int qr = lq < rows ? lq : 0;                   // columns past the rows repeat the first and are dropped
+    float m = -INFINITY, l = 0.f;                            // of the lane's column
+    f32x16 oacc[DB];
+    const int qr = lq < rows ? lq : 0;                       // columns past the rows repeat the first and are dropped
+    if (begin(0) < hi) {
         const int qpos = before + w.by_group.divide(r0 + qr);
-        f32x16 sacc[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[b][r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            // e4m3: step 2x + y takes bytes 8y.. of piece pair x, dims 32x + 16h + 8y ..
-            const int j = E4M3 ? (ks >> 1) * 32 + lh * 16 + (ks & 1) * 8 : ks * 16 + lh * 8;
-            const bf16x8 qf = *reinterpret_cast<const bf16x8*>(&qs[qr][j]);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                bf16x8 kk;
-                if (E4M3) kk = e4m3_to_bf16(kf[b][ks >> 1][2 * (ks & 1)], kf[b][ks >> 1][2 * (ks & 1) + 1]);
-                else kk = *reinterpret_cast<const bf16x8*>(&kf[b][ks]);
-                sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf, sacc[b], 0, 0, 0);
-            }
-        }
-        // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
         const int p_min = before + w.by_group.divide(r0), p_max = before + w.by_group.divide(r0 + rows - 1);
-        if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !there[0] || !there[1]) {
-            const int from = first_seen(qpos, a.window);
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int pos = w0 + b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                    const uint32_t reach = there[b] ? qpos - from + 1 : 0;
-                    sacc[b][r] = (uint32_t)(pos - from) < reach ? sacc[b][r] : -INFINITY;
-                    __builtin_amdgcn_sched_barrier(0);       // one at a time: 32 lane masks do not fit the scalar registers
-                }
-            if (w0 + 64 > hi || w0 < lo || !there[0] || !there[1]) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const uint32_t length = there[b] ? hi - lo : 0;
-                    auto keep = [&](int off) { return (uint32_t)(w0 + 32 * b + 4 * lh + off - lo) < length; };   // inside the block
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int g = 0; g < 2; ++g) {
-                            __builtin_amdgcn_sched_barrier(0);
-                            // positions 16 t + 8 g + 4 lh + 0..3
-                            const int off = 16 * t + 8 * g;
-                            if (E4M3) {
-                                const uint32_t m = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) | (keep(off + 2) ? 0xff0000u : 0) |
-                                                   (keep(off + 3) ? 0xff000000u : 0);
-#pragma unroll
-                                for (int x = 0; x < NF; ++x) vf[b][x][2 * t + g] &= m;
-                            } else {
-                                const uint32_t m0 = (keep(off) ? 0xffffu : 0) | (keep(off + 1) ? 0xffff0000u : 0);
-                                const uint32_t m1 = (keep(off + 2) ? 0xffffu : 0) | (keep(off + 3) ? 0xffff0000u : 0);
-#pragma unroll
-                                for (int db = 0; db < DB; ++db) {
-                                    vf[b][t * DB + db][2 * g] &= m0;
-                                    vf[b][t * DB + db][2 * g + 1] &= m1;
-                                }
-                            }
-                        }
-                }
-            }
-        }
-        float m = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) m = fmaxf(m, sacc[b][r]);
-        m = pair_max(m) * a.scale_log2;                      // scale > 0
-        const float ref = finite_or_0(m);
-        float l = 0.f;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
-                sacc[b][r] = p;
-                l += p;
-            }
-        l = pair_sum(l);
-        f32x16 oacc[DB];
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int step = 0; step < STEPS; ++step) {
+            const int w0 = begin(step), at = AHEAD ? step : 0;
+            if (w0 >= hi) break;                             // wave-uniform
+            const bool whole = id[step][0] >= 0 && id[step][1] >= 0;
+            f32x16 sacc[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                bf16x8 pf;
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[e] = (bf16)sacc[b][8 * t + e];
+                for (int r = 0; r < 16; ++r) sacc[b][r] = 0.f;
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    bf16x8 vv;
-                    if (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
-                    else vv = *reinterpret_cast<const bf16x8*>(&vf[b][t * DB + db]);
-                    oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
+            for (int ks = 0; ks < KS; ++ks) {
+                // e4m3: product 2x + y takes bytes 8y.. of piece pair x, dims 32x + 16h + 8y ..
+                const int j = E4M3 ? (ks >> 1) * 32 + lh * 16 + (ks & 1) * 8 : ks * 16 + lh * 8;
+                const bf16x8 qf = *reinterpret_cast<const bf16x8*>(&qs[qr][j]);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    bf16x8 kk;
+                    if (E4M3) kk = e4m3_to_bf16(kf[at][b][ks >> 1][2 * (ks & 1)], kf[at][b][ks >> 1][2 * (ks & 1) + 1]);
+                    else kk = *reinterpret_cast<const bf16x8*>(&kf[at][b][ks]);
+                    sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf, sacc[b], 0, 0, 0);
                 }
             }
+            if (!AHEAD && step + 1 < STEPS && begin(step + 1) < hi) load_k(step + 1);
+            // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
+            if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !whole) {
+                const int from = first_seen(qpos, a.window);
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int pos = w0 + b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+                        const uint32_t reach = id[step][b] >= 0 ? qpos - from + 1 : 0;
+                        sacc[b][r] = (uint32_t)(pos - from) < reach ? sacc[b][r] : -INFINITY;
+                        __builtin_amdgcn_sched_barrier(0);   // one at a time: 32 lane masks do not fit the scalar registers
+                    }
+                if (w0 + 64 > hi || w0 < lo || !whole) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t length = id[step][b] >= 0 ? hi - lo : 0;
+                        auto keep = [&](int off) { return (uint32_t)(w0 + 32 * b + 4 * lh + off - lo) < length; };   // inside the block
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int g = 0; g < 2; ++g) {
+                                __builtin_amdgcn_sched_barrier(0);
+                                const int off = 16 * t + 8 * g;      // positions 16 t + 8 g + 4 lh + 0..3
+                                if (E4M3) {
+                                    const uint32_t k4 = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) |
+                                                        (keep(off + 2) ? 0xff0000u : 0) | (keep(off + 3) ? 0xff000000u : 0);
+#pragma unroll
+                                    for (int x = 0; x < NF; ++x) vf[at][b][x][2 * t + g] &= k4;
+                                } else {
+                                    const uint32_t m0 = (keep(off) ? 0xffffu : 0) | (keep(off + 1) ? 0xffff0000u : 0);
+                                    const uint32_t m1 = (keep(off + 2) ? 0xffffu : 0) | (keep(off + 3) ? 0xffff0000u : 0);
+#pragma unroll
+                                    for (int db = 0; db < DB; ++db) {
+                                        vf[at][b][t * DB + db][2 * g] &= m0;
+                                        vf[at][b][t * DB + db][2 * g + 1] &= m1;
+                                    }
+                                }
+                            }
+                    }
+                }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[b][r]);
+            mx = fmaxf(m, pair_max(mx) * a.scale_log2);      // scale > 0
+            const float ref = finite_or_0(mx);
+            if (step > 0) {
+                const float alpha = exp2_flush(m - ref);
+                l *= alpha;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+            }
+            m = mx;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
+                    sacc[b][r] = p;
+                    l += p;
+                }
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bf16x8 pf;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) pf[x] = (bf16)sacc[b][8 * t + x];
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        bf16x8 vv;
+                        if (E4M3) vv = e4m3_to_bf16(vf[at][b][db][2 * t], vf[at][b][db][2 * t + 1]);
+                        else vv = *reinterpret_cast<const bf16x8*>(&vf[at][b][t * DB + db]);
+                        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
+                    }
+                }
+            if (!AHEAD && step + 1 < STEPS && begin(step + 1) < hi) load_v(step + 1);
+        }
+        l = pair_sum(l);
         if (lq < rows) {
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -408,7 +446,8 @@ __global__ __launch_bounds__(D) void paged_narrow_join_kernel(PagedQuery a, Page
     const int s = bv.decode_seqs[i];
     const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
     if (token >= n) return;
-    int nch = (before + n - (first_seen(before, a.window) & ~63) + kDecodeChunk - 1) / kDecodeChunk;
+    const int ch = kDecodeChunk * w.steps;
+    int nch = (before + n - (first_seen(before, a.window) & ~63) + ch - 1) / ch;
     if (nch == 1) return;                                    // the output is there
     if (nch > w.max_chunks) nch = w.max_chunks;
     const float* base = partial + partial_at(w, bv.n_decode, i, token, a.Hq, h, 0, D);
@@ -788,9 +827,15 @@ template <int D, bool E4M3>
 static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView& bv, const PagedView& kv, float* ws, hipStream_t st) {
     const int n_narrow = bv.n_decode + w.n_short;
     if (n_narrow > 0) {
-        constexpr int WAVES = E4M3 ? 3 : D == 128 ? 2 : 4;
+        // waves per SIMD: what the registers, and with 32 rows the LDS, leave room for; two for bf16 of d = 128, where a third
+        // keeps the memory streams in shorter runs
+        constexpr int FEW = E4M3 ? (D == 128 ? 3 : 4) : D == 128 ? 2 : 4;
         const unsigned grid = (unsigned)((w.list + (n_narrow - w.first) * w.chunks) * kv.Hkv * w.col_tiles);
-        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, WAVES> : paged_narrow_kernel<D, E4M3, kNarrowRows, 2>;
+        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, 1, FEW>
+                    : w.steps == 1     ? paged_narrow_kernel<D, E4M3, kNarrowRows, 1, 2>
+                                       : paged_narrow_kernel<D, E4M3, kNarrowRows, 2, 2>;
+        if constexpr (E4M3)                                  // eight rows of bf16 leave little behind
+            if (w.narrow_rows <= 8 && w.steps == 2) kern = paged_narrow_kernel<D, E4M3, 8, 2, D == 128 ? 2 : 3>;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
         if (w.max_chunks > 1) {
             const unsigned tokens = (unsigned)(bv.n_decode + w.n_short * w.short_tokens);
