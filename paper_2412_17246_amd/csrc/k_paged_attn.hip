@@ -121,10 +121,14 @@ struct RowSoftmax {
 
 __device__ __forceinline__ int first_seen(int pos, int window) { return window && pos + 1 > window ? pos + 1 - window : 0; }
 
-// Place of a narrow sequence's tokens among the partial results: single tokens first, then `short_tokens` per sequence.
-__device__ __forceinline__ size_t partial_at(const PagedWork& w, int n_decode, int i, int token, int Hq, int head, int chunk, int D) {
+// Partial results of narrow sequences: per (token, query head) and chunk D floats of the output, and behind all of those maximum and
+// sum.  Single tokens come first, then `short_tokens` per sequence.
+__device__ __forceinline__ size_t partial_at(const PagedWork& w, int n_decode, int i, int token, int Hq, int head, int chunk) {
     const int t = i < n_decode ? i : n_decode + (i - n_decode) * w.short_tokens + token;
-    return (((size_t)t * Hq + head) * w.max_chunks + chunk) * (D + 2);
+    return ((size_t)t * Hq + head) * w.max_chunks + chunk;
+}
+__device__ __forceinline__ float2* partial_sums(float* partial, const PagedWork& w, int n_decode, int Hq, int D) {
+    return reinterpret_cast<float2*>(partial + (size_t)(n_decode + w.n_short * w.short_tokens) * Hq * w.max_chunks * D);
 }
 
 }  // namespace
@@ -136,18 +140,18 @@ __device__ __forceinline__ size_t partial_at(const PagedWork& w, int n_decode, i
 // LDS in wave order.  Bound by the cache's bytes.
 //
 // A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d * STEPS cache elements: a sixteenth of the
-// bytes for eight rows of e4m3, an eighth for 32 rows of bf16, at one step.  With two steps half of that; the second step's K is
-// requested when the first step's has been used, its V likewise (AHEAD: both steps before anything, where e4m3 leaves the registers).
+// bytes for eight rows of e4m3 at one step.  Its workgroups take two steps where there are enough of them; the second step's K is
+// requested when the first step's has been used, its V likewise (32 sequences of up to 12000 positions on 8 kv heads with eight query
+// heads each: 80 -> 71 us, and the join 10.7 -> 8.1).  bf16 gains nothing from it (drafts of 3 to 8 tokens 47.4 and 47.8 us).
 // ---------------------------------------------------------------------------------------------
 template <int D, bool E4M3, int RT, int STEPS, int WAVES>
 __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(256) void paged_narrow_kernel(
     PagedQuery a, PagedWork w, BatchView bv, PagedView kv, float* __restrict__ partial) {
     constexpr int CH = kDecodeChunk * STEPS, KS = D / 16, DB = D / 32, LD = D + 8;
     constexpr int NF = E4M3 ? D / 32 : D / 16;               // 16-byte loads per lane and block, of K and again of V
-    constexpr bool AHEAD = E4M3 && STEPS == 2;
-    constexpr int SETS = AHEAD ? 2 : 1;
     __shared__ float wmx[4][RT], wsum[4][RT];
-    __shared__ float osh[4][RT][D];
+    constexpr int PARTS = RT > 8 ? 2 : 1, DP = D / PARTS;    // of the head dim that are merged at a time: LDS for one workgroup more
+    __shared__ float osh[4][RT][DP];
     __shared__ __attribute__((aligned(16))) bf16 qs[RT][LD];
 
     const int G = w.by_group.d;
@@ -225,13 +229,13 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     };
     // pieces of K: [piece][position]; a step takes two, one per lane half.  Pieces of V: [2t + h][j], or [h][j] with both t.
     const int lane_k = (lh * 32 + lq) * 16, lane_v = (lh * D + lq) * 16;
-    u32x4 kf[SETS][2][NF], vf[SETS][2][NF];
+    u32x4 kf[2][NF], vf[2][NF];
     auto load_k = [&](int step) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const __amdgpu_buffer_rsrc_t r = block(kv.k, step, b);
 #pragma unroll
-            for (int x = 0; x < NF; ++x) kf[AHEAD ? step : 0][b][x] = load(r, lane_k, x * 1024);
+            for (int x = 0; x < NF; ++x) kf[b][x] = load(r, lane_k, x * 1024);
         }
     };
     auto load_v = [&](int step) {
@@ -239,15 +243,13 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
         for (int b = 0; b < 2; ++b) {
             const __amdgpu_buffer_rsrc_t r = block(kv.v, step, b);
 #pragma unroll
-            for (int x = 0; x < NF; ++x) vf[AHEAD ? step : 0][b][x] = load(r, lane_v, E4M3 ? x * 512 : (x / DB) * (2 * D * 16) + (x % DB) * 512);
+            for (int x = 0; x < NF; ++x) vf[b][x] = load(r, lane_v, E4M3 ? x * 512 : (x / DB) * (2 * D * 16) + (x % DB) * 512);
         }
     };
-#pragma unroll
-    for (int x = 0; x < SETS; ++x)
-        if (begin(x) < hi) {
-            load_k(x);
-            load_v(x);
-        }
+    if (begin(0) < hi) {
+        load_k(0);
+        load_v(0);
+    }
     __builtin_amdgcn_sched_barrier(0);
     if (a.rope.tab) {
 #pragma unroll
@@ -269,17 +271,17 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 
     float m = -INFINITY, l = 0.f;                            // of the lane's column
     f32x16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
     const int qr = lq < rows ? lq : 0;                       // columns past the rows repeat the first and are dropped
     if (begin(0) < hi) {
         const int qpos = before + w.by_group.divide(r0 + qr);
         const int p_min = before + w.by_group.divide(r0), p_max = before + w.by_group.divide(r0 + rows - 1);
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-#pragma unroll
         for (int step = 0; step < STEPS; ++step) {
-            const int w0 = begin(step), at = AHEAD ? step : 0;
+            const int w0 = begin(step);
             if (w0 >= hi) break;                             // wave-uniform
             const bool whole = id[step][0] >= 0 && id[step][1] >= 0;
             f32x16 sacc[2];
@@ -295,12 +297,12 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     bf16x8 kk;
-                    if (E4M3) kk = e4m3_to_bf16(kf[at][b][ks >> 1][2 * (ks & 1)], kf[at][b][ks >> 1][2 * (ks & 1) + 1]);
-                    else kk = *reinterpret_cast<const bf16x8*>(&kf[at][b][ks]);
+                    if (E4M3) kk = e4m3_to_bf16(kf[b][ks >> 1][2 * (ks & 1)], kf[b][ks >> 1][2 * (ks & 1) + 1]);
+                    else kk = *reinterpret_cast<const bf16x8*>(&kf[b][ks]);
                     sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf, sacc[b], 0, 0, 0);
                 }
             }
-            if (!AHEAD && step + 1 < STEPS && begin(step + 1) < hi) load_k(step + 1);
+            if (step + 1 < STEPS && begin(step + 1) < hi) load_k(step + 1);
             // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
             if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !whole) {
                 const int from = first_seen(qpos, a.window);
@@ -328,14 +330,14 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
                                     const uint32_t k4 = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) |
                                                         (keep(off + 2) ? 0xff0000u : 0) | (keep(off + 3) ? 0xff000000u : 0);
 #pragma unroll
-                                    for (int x = 0; x < NF; ++x) vf[at][b][x][2 * t + g] &= k4;
+                                    for (int x = 0; x < NF; ++x) vf[b][x][2 * t + g] &= k4;
                                 } else {
                                     const uint32_t m0 = (keep(off) ? 0xffffu : 0) | (keep(off + 1) ? 0xffff0000u : 0);
                                     const uint32_t m1 = (keep(off + 2) ? 0xffffu : 0) | (keep(off + 3) ? 0xffff0000u : 0);
 #pragma unroll
                                     for (int db = 0; db < DB; ++db) {
-                                        vf[at][b][t * DB + db][2 * g] &= m0;
-                                        vf[at][b][t * DB + db][2 * g + 1] &= m1;
+                                        vf[b][t * DB + db][2 * g] &= m0;
+                                        vf[b][t * DB + db][2 * g + 1] &= m1;
                                     }
                                 }
                             }
@@ -376,107 +378,117 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 #pragma unroll
                     for (int db = 0; db < DB; ++db) {
                         bf16x8 vv;
-                        if (E4M3) vv = e4m3_to_bf16(vf[at][b][db][2 * t], vf[at][b][db][2 * t + 1]);
-                        else vv = *reinterpret_cast<const bf16x8*>(&vf[at][b][t * DB + db]);
+                        if (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
+                        else vv = *reinterpret_cast<const bf16x8*>(&vf[b][t * DB + db]);
                         oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
                     }
                 }
-            if (!AHEAD && step + 1 < STEPS && begin(step + 1) < hi) load_v(step + 1);
+            if (step + 1 < STEPS && begin(step + 1) < hi) load_v(step + 1);
         }
         l = pair_sum(l);
+    }
+    // a wave that had nothing leaves m = -inf, l = 0, o = 0
+    if (lq < rows && lh == 0) {
+        wmx[wave][lq] = m;
+        wsum[wave][lq] = l;
+    }
+    const bool alone = hi - (lo & ~63) <= CH;                // the only chunk: the output itself
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+        if (part) __syncthreads();
         if (lq < rows) {
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+            for (int db = 0; db < DB / PARTS; ++db)
 #pragma unroll
-                for (int r4 = 0; r4 < 4; ++r4)
+                for (int r4 = 0; r4 < 4; ++r4) {
+                    const f32x16& v = oacc[part * (DB / PARTS) + db];
                     *reinterpret_cast<float4*>(&osh[wave][lq][db * 32 + 8 * r4 + 4 * lh]) =
-                        make_float4(oacc[db][4 * r4], oacc[db][4 * r4 + 1], oacc[db][4 * r4 + 2], oacc[db][4 * r4 + 3]);
-            if (lh == 0) {
-                wmx[wave][lq] = m;
-                wsum[wave][lq] = l;
-            }
+                        make_float4(v[4 * r4], v[4 * r4 + 1], v[4 * r4 + 2], v[4 * r4 + 3]);
+                }
         }
-    } else {
-        for (int x = lane; x < rows * D; x += 64) osh[wave][x / D][x % D] = 0.f;
-        if (lane < rows) {
-            wmx[wave][lane] = -INFINITY;
-            wsum[wave][lane] = 0.f;
-        }
-    }
-    __syncthreads();
-    const bool alone = hi - (lo & ~63) <= CH;                // the only chunk: the output itself
-    for (int x = tid; x < rows * D; x += 256) {
-        const int g = x / D, dd = x - g * D;
-        const float M = fmaxf(fmaxf(wmx[0][g], wmx[1][g]), fmaxf(wmx[2][g], wmx[3][g]));
-        const float ref = finite_or_0(M);
-        float acc = 0.f, L = 0.f;
+        __syncthreads();
+        for (int x = tid * 4; x < rows * DP; x += 1024) {
+            const int g = x / DP, dd = x - g * DP;
+            const float M = fmaxf(fmaxf(wmx[0][g], wmx[1][g]), fmaxf(wmx[2][g], wmx[3][g]));
+            const float ref = finite_or_0(M);
+            float L = 0.f;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const float f = exp2f(wmx[v][g] - ref);
-            acc = fmaf(osh[v][g][dd], f, acc);
-            L = fmaf(wsum[v][g], f, L);
-        }
-        const int t = w.by_group.divide(r0 + g), head = kvh * G + (r0 + g) - t * G;
-        if (alone) {
-            a.out[(size_t)(q0 + t) * a.out_stride + head * D + dd] = (bf16)(L > 0.f ? acc / L * kv.v_scale : 0.f);
-        } else {
-            float* pp = partial + partial_at(w, bv.n_decode, i, t, a.Hq, head, chunk, D);
-            pp[dd] = acc;
-            if (dd == 0) {
-                pp[D] = M;
-                pp[D + 1] = L;
+            for (int v = 0; v < 4; ++v) {
+                const float f = exp2_flush(wmx[v][g] - ref);
+                const f32x4 y = *reinterpret_cast<const f32x4*>(&osh[v][g][dd]);
+#pragma unroll
+                for (int z = 0; z < 4; ++z) acc[z] = fmaf(y[z], f, acc[z]);
+                L = fmaf(wsum[v][g], f, L);
+            }
+            const int t = w.by_group.divide(r0 + g), head = kvh * G + (r0 + g) - t * G, j = part * DP + dd;
+            if (alone) {
+                const float inv = L > 0.f ? kv.v_scale / L : 0.f;
+                const bf16x4 y = {(bf16)(acc[0] * inv), (bf16)(acc[1] * inv), (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+                *reinterpret_cast<bf16x4*>(a.out + (size_t)(q0 + t) * a.out_stride + head * D + j) = y;
+            } else {
+                const size_t at = partial_at(w, bv.n_decode, i, t, a.Hq, head, chunk);
+                *reinterpret_cast<f32x4*>(partial + at * D + j) = acc;
+                if (j == 0) partial_sums(partial, w, bv.n_decode, a.Hq, D)[at] = make_float2(M, L);
             }
         }
     }
 }
 
-// Joins the chunks of the narrow sequences that have several, in increasing order: one workgroup per (token, query head), one
-// thread per head dim, sixteen chunks' loads in flight at once.
+// Joins the chunks of the narrow sequences that have several, in increasing order: D / 4 threads per (token, query head), eight
+// chunks' loads in flight at once.  Bound by the launch and two trips to memory.
+constexpr int kJoinThreads = 128;
 template <int D>
-__global__ __launch_bounds__(D) void paged_narrow_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
-                                                              const float* __restrict__ partial) {
-    constexpr int NB = 16;
+__global__ __launch_bounds__(kJoinThreads) void paged_narrow_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
+                                                                         float* __restrict__ partial) {
+    constexpr int NB = 8, TPR = D / 4;
     int i = blockIdx.x, token = 0;
     if (i >= bv.n_decode) {
         const int x = i - bv.n_decode;
         i = bv.n_decode + x / w.short_tokens;
         token = x % w.short_tokens;
     }
-    const int h = blockIdx.y, dd = threadIdx.x;
+    const int h = blockIdx.y * (kJoinThreads / TPR) + threadIdx.x / TPR, j = (threadIdx.x % TPR) * 4;
     const int s = bv.decode_seqs[i];
     const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
-    if (token >= n) return;
+    if (token >= n || h >= a.Hq) return;
     const int ch = kDecodeChunk * w.steps;
     int nch = (before + n - (first_seen(before, a.window) & ~63) + ch - 1) / ch;
     if (nch == 1) return;                                    // the output is there
     if (nch > w.max_chunks) nch = w.max_chunks;
-    const float* base = partial + partial_at(w, bv.n_decode, i, token, a.Hq, h, 0, D);
-    float M = -INFINITY, num = 0.f, den = 0.f;
+    const size_t at = partial_at(w, bv.n_decode, i, token, a.Hq, h, 0);
+    const float* o = partial + at * D + j;
+    const float2* ml = partial_sums(partial, w, bv.n_decode, a.Hq, D) + at;
+    float M = -INFINITY, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
     for (int c0 = 0; c0 < nch; c0 += NB) {
-        float mv[NB], ov[NB], lv[NB];
+        float2 mv[NB];
+        f32x4 ov[NB];
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
-            const float* pc = base + (size_t)(c0 + u < nch ? c0 + u : nch - 1) * (D + 2);
-            mv[u] = pc[D];
-            ov[u] = pc[dd];
-            lv[u] = pc[D + 1];
+            const int c = c0 + u < nch ? c0 + u : nch - 1;
+            mv[u] = ml[c];
+            ov[u] = *reinterpret_cast<const f32x4*>(o + (size_t)c * D);
         }
         float Mb = M;
 #pragma unroll
-        for (int u = 0; u < NB; ++u) Mb = fmaxf(Mb, mv[u]);
-        const float ref = finite_or_0(Mb), keep = exp2f(M - ref);
+        for (int u = 0; u < NB; ++u) Mb = fmaxf(Mb, mv[u].x);
+        const float ref = finite_or_0(Mb), keep = exp2_flush(M - ref);
         num *= keep;
         den *= keep;
         M = Mb;
         // no branches: behind one every load would be waited for by itself.  A chunk past the end gets weight zero.
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
-            const float f = c0 + u < nch ? exp2f(mv[u] - ref) : 0.f;
-            num = fmaf(ov[u], f, num);
-            den = fmaf(lv[u], f, den);
+            const float f = c0 + u < nch ? exp2_flush(mv[u].x - ref) : 0.f;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) num[z] = fmaf(ov[u][z], f, num[z]);
+            den = fmaf(mv[u].y, f, den);
         }
     }
-    a.out[(size_t)(q0 + token) * a.out_stride + h * D + dd] = (bf16)(den > 0.f ? num / den * kv.v_scale : 0.f);
+    const float inv = den > 0.f ? kv.v_scale / den : 0.f;
+    const bf16x4 y = {(bf16)(num[0] * inv), (bf16)(num[1] * inv), (bf16)(num[2] * inv), (bf16)(num[3] * inv)};
+    *reinterpret_cast<bf16x4*>(a.out + (size_t)(q0 + token) * a.out_stride + h * D + j) = y;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -831,15 +843,15 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
         // keeps the memory streams in shorter runs
         constexpr int FEW = E4M3 ? (D == 128 ? 3 : 4) : D == 128 ? 2 : 4;
         const unsigned grid = (unsigned)((w.list + (n_narrow - w.first) * w.chunks) * kv.Hkv * w.col_tiles);
-        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, 1, FEW>
-                    : w.steps == 1     ? paged_narrow_kernel<D, E4M3, kNarrowRows, 1, 2>
-                                       : paged_narrow_kernel<D, E4M3, kNarrowRows, 2, 2>;
-        if constexpr (E4M3)                                  // eight rows of bf16 leave little behind
-            if (w.narrow_rows <= 8 && w.steps == 2) kern = paged_narrow_kernel<D, E4M3, 8, 2, D == 128 ? 2 : 3>;
+        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, 1, FEW> : paged_narrow_kernel<D, E4M3, kNarrowRows, 1, 3>;
+        if constexpr (E4M3)                                  // bf16 takes one step always
+            if (w.steps == 2)
+                kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, 2, D == 128 ? 3 : 4> : paged_narrow_kernel<D, E4M3, kNarrowRows, 2, 3>;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
         if (w.max_chunks > 1) {
             const unsigned tokens = (unsigned)(bv.n_decode + w.n_short * w.short_tokens);
-            hipLaunchKernelGGL(paged_narrow_join_kernel<D>, dim3(tokens, q.Hq), dim3(D), 0, st, q, w, bv, kv, ws);
+            constexpr int HEADS = kJoinThreads / (D / 4);    // of one workgroup
+            hipLaunchKernelGGL(paged_narrow_join_kernel<D>, dim3(tokens, (q.Hq + HEADS - 1) / HEADS), dim3(kJoinThreads), 0, st, q, w, bv, kv, ws);
         }
     }
     if (w.wide_units > 0) {

@@ -89,8 +89,7 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
     w.col_tiles = (std::max(G, 1) + kNarrowRows - 1) / kNarrowRows;
     w.narrow_rows = std::max(std::min(G, kNarrowRows), w.short_tokens * G);
     w.first = window ? 0 : bv.n_decode;
-    // Chunks of two steps, where partial results are more than a sixteenth of what is read and half as many workgroups still fill
-    // the chip
+    // e4m3: chunks of two steps, where half as many workgroups still fill the chip
     auto cut = [&](int steps) {
         int64_t list = 0;
         if (!window)
@@ -105,7 +104,7 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
             for (int s : b->decode_seqs) n += chunks_of(keys_of(b->kv_before[s], 1, window), steps);
         return n * Hkv * w.col_tiles;
     };
-    if (!(w.narrow_rows * (e4m3 ? 2 : 1) > 8 && cut(2) >= 512)) cut(1);
+    if (!e4m3 || cut(2) < 512) cut(1);
     // wide rows: enough ranges of the keys that the chip is full, of four tiles of 64 keys at least
     int64_t units = 0, keys = 0;
     for (int s = 0; s < b->B; ++s) {
