@@ -502,13 +502,18 @@ struct WideUnit {
     int item, sub, split, kvh;
 };
 // XCD-aware: workgroups go to the eight XCDs in turn; with a multiple of eight kv heads each XCD takes whole kv heads and walks
-// one after the other, longest key ranges first, so that what runs on it at a time shares the K and V in its L2.
+// one after the other, longest key ranges first, so that what runs on it at a time shares the K and V in its L2.  A grid that fits the
+// chip in one go, two workgroups per CU, lasts as long as its busiest CU, which holds an XCD's workgroups c and 32 + c: the second half
+// is walked backwards, long with short (one prompt of 2048 tokens on 32 kv heads: 61 -> 49 us).
 __device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int subs, int Hkv, int splits) {
     const int per_head = n_items * subs * splits;
     WideUnit u;
     int rest;
     if ((Hkv & 7) == 0) {
-        const int seq = b >> 3, k = seq / per_head;
+        const int n_x = per_head * (Hkv >> 3);
+        int seq = b >> 3;
+        if (n_x <= 64 && seq >= 32) seq = 32 + (n_x - 1 - seq);
+        const int k = seq / per_head;
         u.kvh = (b & 7) * (Hkv >> 3) + k;
         rest = seq - k * per_head;
     } else {
@@ -522,12 +527,12 @@ __device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int subs, int 
     return u;
 }
 
-// the tiles of 64 keys that `rows` rows from r0 on see, or the range of them that `split` names
+// the tiles of 64 keys that kWideRows rows from r0 on see, or the range of them that `split` names
 struct WideKeys {
     int t0, t1, splits;
 };
-__device__ __forceinline__ WideKeys wide_keys(int before, int r0, int rows, int R, int G, int window, int split, int splits) {
-    const int first = before + r0 / G, last = before + (r0 + rows < R ? r0 + rows - 1 : R - 1) / G;
+__device__ __forceinline__ WideKeys wide_keys(int before, int r0, int R, int G, int window, int split, int splits) {
+    const int first = before + r0 / G, last = before + (r0 + kWideRows < R ? r0 + kWideRows - 1 : R - 1) / G;
     WideKeys k;
     k.t0 = first_seen(first, window) >> 6;
     k.t1 = (last >> 6) + 1;
@@ -562,6 +567,12 @@ struct TileMap {
 template <int D>
 __device__ __forceinline__ size_t block_start(int block) { return (size_t)(uint32_t)(block < 0 ? 0 : block) * (32 * D); }
 
+// Partial results of key ranges: [kv head][range][dims by fours][row of the batch, token * G + query head of the group][4], and behind
+// those maximum and sum, [kv head][range][row][2].
+__device__ __forceinline__ float2* wide_sums(float* partial, size_t rows, int Hkv, int splits, int D) {
+    return reinterpret_cast<float2*>(partial + rows * Hkv * splits * D);
+}
+
 template <int D, bool E4M3, bool ROTATE, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
                                                             float* __restrict__ partial) {
@@ -578,7 +589,7 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s], row = bv.seq_slot[s];
     const int R = n * G, r0 = (qt * G + unit.sub) * kWideRows;
     if (r0 >= R || R <= w.narrow_limit) return;
-    const WideKeys keys = wide_keys(before, r0, kWideRows, R, G, a.window, unit.split, w.splits);
+    const WideKeys keys = wide_keys(before, r0, R, G, a.window, unit.split, w.splits);
     if (SPLIT && keys.t0 >= keys.t1) return;
     const int hi = before + n, lo = first_seen(before + r0 / G, a.window);
     const int kvh = unit.kvh;
@@ -741,15 +752,18 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     const float l = pair_sum(rows.l);
     __builtin_amdgcn_s_waitcnt(0x0070);                      // no LDS write may be in flight when the workgroup ends
     if (SPLIT) {
-        float* base = partial + ((((size_t)unit.item * G + unit.sub) * Hkv + kvh) * w.splits + unit.split) * (kWideRows * (D + 2));
-        float* op = base + wave * 32 * D + lq * 4;           // [dims by fours][row][4]
+        if (valid) {
+            const size_t total = (size_t)bv.T * G, part = ((size_t)kvh * w.splits + unit.split) * total, at = (size_t)q0 * G + r;
+            float* op = partial + (part * (D / 4) + at) * 4;
 #pragma unroll
-        for (int b = 0; b < DB; ++b)
+            for (int b = 0; b < DB; ++b)
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4)
-                *reinterpret_cast<float4*>(op + ((b * 4 + r4) * 2 + lh) * 128) =
-                    make_float4(o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]);
-        if (lh == 0) *reinterpret_cast<float2*>(base + kWideRows * D + (wave * 32 + lq) * 2) = make_float2(rows.seen ? rows.ref : -INFINITY, l);
+                for (int r4 = 0; r4 < 4; ++r4)
+                    *reinterpret_cast<float4*>(op + ((b * 4 + r4) * 2 + lh) * total * 4) =
+                        make_float4(o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]);
+            if (lh == 0)
+                wide_sums(partial, total, Hkv, w.splits, D)[part + at] = make_float2(rows.seen ? rows.ref : -INFINITY, l);
+        }
     } else if (valid) {
         const float inv = l > 0.f ? kv.v_scale / l : 0.f;
         int at = rc;
@@ -768,47 +782,42 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     }
 }
 
-// Joins the key ranges of wide rows, in increasing order: one workgroup per 32 rows.
+// Joins the key ranges of wide rows, in increasing order: one workgroup per 32 rows of a kv head.
 template <int D>
 __global__ __launch_bounds__(256) void paged_wide_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
-                                                              const float* __restrict__ partial) {
-    const int Hkv = kv.Hkv, G = a.Hq / Hkv;
-    const int part = blockIdx.x & 3, b = blockIdx.x >> 2;
-    const int kvh = b % Hkv, sub = b / Hkv % G, item = b / Hkv / G;
-    const int s = bv.prefill_items[2 * item], qt = bv.prefill_items[2 * item + 1];
-    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
-    const int R = n * G, r0 = (qt * G + sub) * kWideRows;
-    const int x = part * 32 + (threadIdx.x & 31), r = r0 + x;
-    if (r >= R || R <= w.narrow_limit) return;
-    const WideKeys keys = wide_keys(before, r0, kWideRows, R, G, a.window, 0, w.splits);
-    const float* base = partial + (((size_t)item * G + sub) * Hkv + kvh) * w.splits * (kWideRows * (D + 2));
-    constexpr size_t UNIT = kWideRows * (D + 2);
+                                                              float* __restrict__ partial) {
+    const int Hkv = kv.Hkv, G = w.by_group.d, kvh = blockIdx.y;
+    const int64_t total = (int64_t)bv.T * G, at = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    if (at >= total) return;
+    const int t = w.by_group.divide((int)at), s = bv.token_seq[t], q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0;
+    const int R = n * G, r = (int)at - q0 * G;
+    if (n < 2 || R <= w.narrow_limit) return;
+    const WideKeys keys = wide_keys(bv.kv_before[s], r & ~(kWideRows - 1), R, G, a.window, 0, w.splits);
+    const float2* ml = wide_sums(partial, total, Hkv, w.splits, D) + (size_t)kvh * w.splits * total + at;
+    const float* o = partial + ((size_t)kvh * w.splits * total * (D / 4) + at) * 4;
     float M = -INFINITY;
-    for (int k = 0; k < keys.splits; ++k) M = fmaxf(M, base[k * UNIT + kWideRows * D + x * 2]);
+    for (int k = 0; k < keys.splits; ++k) M = fmaxf(M, ml[k * total].x);
     const float ref = finite_or_0(M);
     constexpr int NQ = D / 32;
-    float4 acc[NQ] = {};
+    f32x4 acc[NQ] = {};
     float L = 0.f;
     for (int k = 0; k < keys.splits; ++k) {
-        const float* pk = base + k * UNIT;
-        const float2 ml = *reinterpret_cast<const float2*>(pk + kWideRows * D + x * 2);
-        const float f = exp2f(ml.x - ref);
-        L = fmaf(ml.y, f, L);
+        const float2 x = ml[k * total];
+        const float f = exp2_flush(x.x - ref);
+        L = fmaf(x.y, f, L);
+        const float* ok = o + (size_t)k * total * D;
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(pk + part * 32 * D + (i * 8 + (threadIdx.x >> 5)) * 128 + (threadIdx.x & 31) * 4);
-            acc[i].x = fmaf(v.x, f, acc[i].x);
-            acc[i].y = fmaf(v.y, f, acc[i].y);
-            acc[i].z = fmaf(v.z, f, acc[i].z);
-            acc[i].w = fmaf(v.w, f, acc[i].w);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(ok + (size_t)(i * 8 + (threadIdx.x >> 5)) * total * 4);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) acc[i][z] = fmaf(v[z], f, acc[i][z]);
         }
     }
     const float inv = L > 0.f ? kv.v_scale / L : 0.f;
-    const int token = r / G, head = kvh * G + r - token * G;
-    bf16* op = a.out + (size_t)(q0 + token) * a.out_stride + head * D + (threadIdx.x >> 5) * 4;
+    bf16* op = a.out + (size_t)t * a.out_stride + (kvh * G + (int)at - t * G) * D + (threadIdx.x >> 5) * 4;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        const bf16x4 v = {(bf16)(acc[i].x * inv), (bf16)(acc[i].y * inv), (bf16)(acc[i].z * inv), (bf16)(acc[i].w * inv)};
+        const bf16x4 v = {(bf16)(acc[i][0] * inv), (bf16)(acc[i][1] * inv), (bf16)(acc[i][2] * inv), (bf16)(acc[i][3] * inv)};
         *reinterpret_cast<bf16x4*>(op + i * 32) = v;
     }
 }
@@ -821,7 +830,7 @@ static size_t narrow_bytes(const PagedWork& w, const BatchView& bv, int Hq, int 
 }
 
 size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, int, int d) {
-    const size_t wide = w.splits > 1 ? (size_t)bv.n_prefill_items * Hq * w.splits * kWideRows * (d + 2) * sizeof(float) : 0;
+    const size_t wide = w.splits > 1 ? (size_t)bv.T * Hq * w.splits * (d + 2) * sizeof(float) : 0;
     return narrow_bytes(w, bv, Hq, d) + wide;
 }
 
@@ -832,7 +841,7 @@ static void launch_wide(const PagedQuery& q, const PagedWork& w, const BatchView
     (void)limit.raise(reinterpret_cast<const void*>(paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), kLds);
     hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), dim3((unsigned)(bv.n_prefill_items * q.Hq * w.splits)), dim3(256), kLds, st, q,
                        w, bv, kv, ws);
-    if (SPLIT) hipLaunchKernelGGL(paged_wide_join_kernel<D>, dim3((unsigned)(bv.n_prefill_items * q.Hq * 4)), dim3(256), 0, st, q, w, bv, kv, ws);
+    if (SPLIT) hipLaunchKernelGGL(paged_wide_join_kernel<D>, dim3((unsigned)(((int64_t)bv.T * w.by_group.d + 31) / 32), kv.Hkv), dim3(256), 0, st, q, w, bv, kv, ws);
 }
 
 template <int D, bool E4M3>

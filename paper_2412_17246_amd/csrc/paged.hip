@@ -105,7 +105,6 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
         return n * Hkv * w.col_tiles;
     };
     if (!e4m3 || cut(2) < 512) cut(1);
-    // wide rows: enough ranges of the keys that the chip is full, of four tiles of 64 keys at least
     int64_t units = 0, keys = 0;
     for (int s = 0; s < b->B; ++s) {
         const int n = b->q_start[s + 1] - b->q_start[s];
@@ -114,7 +113,14 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
         units += (rows + kWideRows - 1) / kWideRows * Hkv;
         keys = std::max(keys, keys_of((int64_t)b->kv_before[s] + n - std::min<int64_t>(n, kWideRows / G + 1), std::min<int64_t>(n, kWideRows / G + 1), window));
     }
-    w.splits = units ? (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / units, 16), keys / 256)) : 1;
+    // Ranges of the keys: one workgroup per CU, or two where a range keeps twelve tiles of 64 keys.  Two on a CU run a quarter faster
+    // than one, but every range costs its rows' partial results twice; and one range, which needs none, has a launch less, too.
+    // (us with 256 / 512 workgroups: 128 rows on 8000 keys 33 / 40, 512 on 3001 46 / 45, 16 drafts of 10 to 16 tokens 70 / 57,
+    // 1000 rows on 2000 keys, 250 workgroups in one range, 54 / 57.)
+    const int64_t tiles = (keys + 63) / 64;
+    const auto ranges = [&](int64_t n) { return units ? std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(n / units, 16), tiles / 4)) : 1; };
+    w.splits = (int)ranges(256);
+    if (tiles >= 12 * ranges(512) && (w.splits > 1 || tiles >= 64)) w.splits = (int)ranges(512);
     w.wide_units = (int)std::min<int64_t>(units, 0x7fffffff);
     w.by_heads = divisor(Hkv * w.col_tiles);
     w.by_chunks = divisor(std::max(w.chunks, 1));
