@@ -210,8 +210,7 @@ struct BatchView {
     int decode_chunks;             // upper bound on ceil((kv_before+1)/kDecodeChunk) over decode seqs
     // One entry (two int4) per (decode sequence, chunk of its cache) that exists now, sequence by
     // sequence: (sequence index, KV slot, index into decode_seqs, chunks of this sequence), (index of
-    // the sequence's first entry, then, for pair i of two chunks next to each other, counted through the sequences in the same order:
-    // the index into decode_seqs of the pair's sequence and that sequence's first pair, 0).  The decode attention runs n_decode_work * Hkv workgroups;
+    // the sequence's first entry, 0, 0, 0).  The decode attention runs n_decode_work * Hkv workgroups;
     // workgroup b reads entry b / Hkv, which belongs to the right sequence, and takes
     // (kv head, chunk) = divmod(b - Hkv * first, chunks): a sequence's kv heads one after the other,
     // each head's chunks in order, which is the order the cache lies in memory.

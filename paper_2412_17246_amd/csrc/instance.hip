@@ -7,7 +7,6 @@
 
 #include <new>
 #include <string>
-#include <utility>
 #include <vector>
 
 #include "few_rows.h"
@@ -787,20 +786,14 @@ int describe_batch(const bz_batch_desc* d, bz_batch* b, std::vector<int32_t>& im
     // room for kWorkGrowth more chunks per sequence as bz_batch_advance lengthens the caches.  The room is
     // zero-filled, so that a kernel that ran ahead of an update would read a harmless entry, never garbage.
     std::vector<int32_t> work;
-    std::vector<std::pair<int32_t, int32_t>> pairs;          // (index into decode_seqs, first pair) of every pair of chunks
     for (int di = 0; di < b->n_decode; ++di) {
         const int s = b->decode_seqs[di];
         const int n = (b->kv_before[s] + 1 + kDecodeChunk - 1) / kDecodeChunk;
-        const int first = (int)(work.size() / 8), first_pair = (int)pairs.size();
+        const int first = (int)(work.size() / 8);
         for (int c = 0; c < n; ++c) {
             const int32_t entry[8] = {s, b->seq_slot[s], di, n, first, 0, 0, 0};
             work.insert(work.end(), entry, entry + 8);
-            if (c % 2 == 0) pairs.push_back({di, first_pair});
         }
-    }
-    for (size_t i = 0; i < pairs.size(); ++i) {              // never more than entries
-        work[8 * i + 5] = pairs[i].first;
-        work[8 * i + 6] = pairs[i].second;
     }
     const size_t present = work.size() / 8;
     size_t n_i32 = (size_t)(B + 1) + B + B + T + items.size() + b->decode_seqs.size();

@@ -119,6 +119,11 @@ struct RowSoftmax {
     }
 };
 
+// x of the lane plus x of the lane eight further in its row of sixteen
+__device__ __forceinline__ float add_eighth(float x) {
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, true));
+}
+
 __device__ __forceinline__ int first_seen(int pos, int window) { return window && pos + 1 > window ? pos + 1 - window : 0; }
 
 // Partial results of narrow sequences: per (token, query head) and chunk D floats of the output, and behind all of those maximum and
@@ -134,25 +139,30 @@ __device__ __forceinline__ float2* partial_sums(float* partial, const PagedWork&
 }  // namespace
 
 // ---------------------------------------------------------------------------------------------
-// Narrow: a workgroup reads one chunk of 256 * STEPS positions of one kv head once, for up to RT rows.  Each of its four waves takes
-// 64 positions at a time, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose
+// Narrow: a workgroup reads one chunk of 256 positions of one kv head once, for up to RT rows.  Each of its four waves takes 64
+// positions, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose
 // row operand is the cache as it lies in memory; rows of the problem are the 32 columns.  The four waves' results are merged through
 // LDS in wave order.  Bound by the cache's bytes.
 //
-// A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d * STEPS cache elements: a sixteenth of the
-// bytes for eight rows of e4m3 at one step.  Its workgroups take two steps where there are enough of them; the second step's K is
-// requested when the first step's has been used, its V likewise (32 sequences of up to 12000 positions on 8 kv heads with eight query
-// heads each: 80 -> 71 us, and the join 10.7 -> 8.1).  bf16 gains nothing from it (drafts of 3 to 8 tokens 47.4 and 47.8 us).
-// ---------------------------------------------------------------------------------------------
-template <int D, bool E4M3, int RT, int STEPS, int WAVES>
+// Queries are kept as the sum of two bf16, rounded after the rotation to 16 bits and not to 8: what the matrix pipe does beside the
+// stream costs little.  With up to eight rows the second parts are columns 8..15, which the first parts leave free, and the scores'
+// two parts are added across lanes; with more they are products of their own.  The output's distance from a computation in 64 bits is
+// 2.2e-3 that way (rms, bf16's own rounding of the output 1.7e-3), against 2.7e-3 with queries of one bf16; the rest is the weights,
+// which are rounded to bf16 for the product.
+//
+// A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d cache elements: a sixteenth of the bytes
+// for eight rows of e4m3.  Chunks of twice the length halve that and gain nothing (32 sequences of up to 12000 positions on 8 kv heads
+// with eight query heads each, kernel and join: 81.3 us with one step of 64 positions per wave and four waves per SIMD, 83.8 with two
+// steps and the three waves that these leave room for).
+template <int D, bool E4M3, int RT, int WAVES>
 __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(256) void paged_narrow_kernel(
     PagedQuery a, PagedWork w, BatchView bv, PagedView kv, float* __restrict__ partial) {
-    constexpr int CH = kDecodeChunk * STEPS, KS = D / 16, DB = D / 32, LD = D + 8;
+    constexpr int CH = kDecodeChunk, KS = D / 16, DB = D / 32, LD = D + 8;
     constexpr int NF = E4M3 ? D / 32 : D / 16;               // 16-byte loads per lane and block, of K and again of V
     __shared__ float wmx[4][RT], wsum[4][RT];
     constexpr int PARTS = RT > 8 ? 2 : 1, DP = D / PARTS;    // of the head dim that are merged at a time: LDS for one workgroup more
     __shared__ float osh[4][RT][DP];
-    __shared__ __attribute__((aligned(16))) bf16 qs[RT][LD];
+    __shared__ __attribute__((aligned(16))) bf16 qs[2][RT][LD];
 
     const int G = w.by_group.d;
     // kv heads next to each other, then chunks, then sequences: the order in which pages lie in memory
@@ -160,19 +170,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     const int hc = blockIdx.x - e * w.by_heads.d, kvh = w.by_tiles.divide(hc), ct = hc - kvh * w.by_tiles.d;
     int i, s, row, chunk;
     if (e < w.list) {
-        const int4 of = bv.decode_work[2 * e + 1];
-        if (STEPS == 1) {
-            const int4 item = bv.decode_work[2 * e];
-            s = item.x;
-            row = item.y;
-            i = item.z;
-            chunk = e - of.x;
-        } else {
-            i = of.y;
-            s = bv.decode_seqs[i];
-            row = bv.seq_slot[s];
-            chunk = e - of.z;
-        }
+        const int4 item = bv.decode_work[2 * e];
+        s = item.x;
+        row = item.y;
+        i = item.z;
+        chunk = e - bv.decode_work[2 * e + 1].x;
     } else {
         e -= w.list;
         i = w.by_chunks.divide(e);
@@ -190,16 +192,11 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lq = lane & 31, lh = lane >> 5;
-    // positions of a step; wave-uniform
-    auto begin = [&](int step) { return c0 + (step * 4 + wave) * 64; };
-    int id[STEPS][2];                                        // pages, -1 for one that is not there
+    const int w0 = c0 + wave * 64;
+    const bool live = w0 < hi;                               // wave-uniform
+    int id[2];                                               // pages, -1 for one that is not there
 #pragma unroll
-    for (int x = 0; x < STEPS; ++x)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int pos = begin(x) + 32 * b;
-            id[x][b] = pos < hi ? page_of(kv, row, pos) : -1;
-        }
+    for (int b = 0; b < 2; ++b) id[b] = w0 + 32 * b < hi ? page_of(kv, row, w0 + 32 * b) : -1;
 
     // queries: unit = 8 pairs of a row, requested before the stream
     constexpr int UPR = D / 16;
@@ -219,10 +216,10 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 
     // non-temporal: nobody reads them again.  A base in scalar registers, one vector register for all addresses of K, one for V.
     constexpr int EL = E4M3 ? 1 : 2;
-    auto block = [&](void* cache, int step, int b) {
-        const int page = id[step][b] < 0 ? 0 : id[step][b];  // read in bounds, masked below
-        return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(cache) + block_base(kv, page, kvh, begin(step) + 32 * b) * EL, 0,
-                                                 32 * D * EL, 0x00020000);
+    auto block = [&](void* cache, int b) {
+        const int page = id[b] < 0 ? 0 : id[b];              // read in bounds, masked below
+        return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(cache) + block_base(kv, page, kvh, w0 + 32 * b) * EL, 0, 32 * D * EL,
+                                                 0x00020000);
     };
     auto load = [&](__amdgpu_buffer_rsrc_t r, int lane_at, int at) {
         return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 2));
@@ -230,40 +227,47 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     // pieces of K: [piece][position]; a step takes two, one per lane half.  Pieces of V: [2t + h][j], or [h][j] with both t.
     const int lane_k = (lh * 32 + lq) * 16, lane_v = (lh * D + lq) * 16;
     u32x4 kf[2][NF], vf[2][NF];
-    auto load_k = [&](int step) {
+    auto load_k = [&]() {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const __amdgpu_buffer_rsrc_t r = block(kv.k, step, b);
+            const __amdgpu_buffer_rsrc_t r = block(kv.k, b);
 #pragma unroll
             for (int x = 0; x < NF; ++x) kf[b][x] = load(r, lane_k, x * 1024);
         }
     };
-    auto load_v = [&](int step) {
+    auto load_v = [&]() {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const __amdgpu_buffer_rsrc_t r = block(kv.v, step, b);
+            const __amdgpu_buffer_rsrc_t r = block(kv.v, b);
 #pragma unroll
             for (int x = 0; x < NF; ++x) vf[b][x] = load(r, lane_v, E4M3 ? x * 512 : (x / DB) * (2 * D * 16) + (x % DB) * 512);
         }
     };
-    if (begin(0) < hi) {
-        load_k(0);
-        load_v(0);
+    if (live) {
+        load_k();
+        if (RT == 8) load_v();
     }
     __builtin_amdgcn_sched_barrier(0);
+    bf16x8 rlo = {}, rhi = {};                               // the second parts
     if (a.rope.tab) {
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
             const float c = cs[x >> 1][2 * (x & 1)], sn = cs[x >> 1][2 * (x & 1) + 1];
-            const float y = (float)qlo[x], z = (float)qhi[x];
-            qlo[x] = (bf16)(y * c - z * sn);
-            qhi[x] = (bf16)(z * c + y * sn);
+            const float y = (float)qlo[x], z = (float)qhi[x], p = y * c - z * sn, q = z * c + y * sn;
+            qlo[x] = (bf16)p;
+            qhi[x] = (bf16)q;
+            rlo[x] = (bf16)(p - (float)qlo[x]);
+            rhi[x] = (bf16)(q - (float)qhi[x]);
         }
     }
     if (tid < units) {
-        *reinterpret_cast<bf16x8*>(&qs[ur][uj]) = qlo;
-        *reinterpret_cast<bf16x8*>(&qs[ur][D / 2 + uj]) = qhi;
+        *reinterpret_cast<bf16x8*>(&qs[0][ur][uj]) = qlo;
+        *reinterpret_cast<bf16x8*>(&qs[0][ur][D / 2 + uj]) = qhi;
+        *reinterpret_cast<bf16x8*>(&qs[1][ur][uj]) = rlo;
+        *reinterpret_cast<bf16x8*>(&qs[1][ur][D / 2 + uj]) = rhi;
     }
+    // with more queries to keep on the way, V's requests would leave them no registers
+    if (RT > 8 && live) load_v();
     // hand-over through LDS; a full barrier would drain the stream
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
@@ -275,116 +279,111 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-    const int qr = lq < rows ? lq : 0;                       // columns past the rows repeat the first and are dropped
-    if (begin(0) < hi) {
+    // columns past the rows repeat the first and are dropped
+    constexpr bool BESIDE = RT == 8;                         // second parts in columns of their own
+    const int col = BESIDE ? lq & 7 : lq, qr = col < rows ? col : 0;
+    const bf16* qcol = &qs[BESIDE ? (lq >> 3) & 1 : 0][qr][0];
+    if (live) {
         const int qpos = before + w.by_group.divide(r0 + qr);
         const int p_min = before + w.by_group.divide(r0), p_max = before + w.by_group.divide(r0 + rows - 1);
+        const bool whole = id[0] >= 0 && id[1] >= 0;
+        f32x16 sacc[2];
 #pragma unroll
-        for (int step = 0; step < STEPS; ++step) {
-            const int w0 = begin(step);
-            if (w0 >= hi) break;                             // wave-uniform
-            const bool whole = id[step][0] >= 0 && id[step][1] >= 0;
-            f32x16 sacc[2];
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[b][r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            // e4m3: product 2x + y takes bytes 8y.. of piece pair x, dims 32x + 16h + 8y ..
+            const int j = E4M3 ? (ks >> 1) * 32 + lh * 16 + (ks & 1) * 8 : ks * 16 + lh * 8;
+            const bf16x8 qf = *reinterpret_cast<const bf16x8*>(qcol + j);
+            bf16x8 ql;
+            if (!BESIDE) ql = *reinterpret_cast<const bf16x8*>(&qs[1][qr][j]);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                bf16x8 kk;
+                if (E4M3) kk = e4m3_to_bf16(kf[b][ks >> 1][2 * (ks & 1)], kf[b][ks >> 1][2 * (ks & 1) + 1]);
+                else kk = *reinterpret_cast<const bf16x8*>(&kf[b][ks]);
+                sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf, sacc[b], 0, 0, 0);
+                if (!BESIDE) sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, ql, sacc[b], 0, 0, 0);
+            }
+        }
+        if (BESIDE)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sacc[b][r] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                // e4m3: product 2x + y takes bytes 8y.. of piece pair x, dims 32x + 16h + 8y ..
-                const int j = E4M3 ? (ks >> 1) * 32 + lh * 16 + (ks & 1) * 8 : ks * 16 + lh * 8;
-                const bf16x8 qf = *reinterpret_cast<const bf16x8*>(&qs[qr][j]);
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    bf16x8 kk;
-                    if (E4M3) kk = e4m3_to_bf16(kf[b][ks >> 1][2 * (ks & 1)], kf[b][ks >> 1][2 * (ks & 1) + 1]);
-                    else kk = *reinterpret_cast<const bf16x8*>(&kf[b][ks]);
-                    sacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf, sacc[b], 0, 0, 0);
-                }
-            }
-            if (step + 1 < STEPS && begin(step + 1) < hi) load_k(step + 1);
-            // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
-            if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !whole) {
-                const int from = first_seen(qpos, a.window);
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int pos = w0 + b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                        const uint32_t reach = id[step][b] >= 0 ? qpos - from + 1 : 0;
-                        sacc[b][r] = (uint32_t)(pos - from) < reach ? sacc[b][r] : -INFINITY;
-                        __builtin_amdgcn_sched_barrier(0);   // one at a time: 32 lane masks do not fit the scalar registers
-                    }
-                if (w0 + 64 > hi || w0 < lo || !whole) {
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const uint32_t length = id[step][b] >= 0 ? hi - lo : 0;
-                        auto keep = [&](int off) { return (uint32_t)(w0 + 32 * b + 4 * lh + off - lo) < length; };   // inside the block
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-#pragma unroll
-                            for (int g = 0; g < 2; ++g) {
-                                __builtin_amdgcn_sched_barrier(0);
-                                const int off = 16 * t + 8 * g;      // positions 16 t + 8 g + 4 lh + 0..3
-                                if (E4M3) {
-                                    const uint32_t k4 = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) |
-                                                        (keep(off + 2) ? 0xff0000u : 0) | (keep(off + 3) ? 0xff000000u : 0);
-#pragma unroll
-                                    for (int x = 0; x < NF; ++x) vf[b][x][2 * t + g] &= k4;
-                                } else {
-                                    const uint32_t m0 = (keep(off) ? 0xffffu : 0) | (keep(off + 1) ? 0xffff0000u : 0);
-                                    const uint32_t m1 = (keep(off + 2) ? 0xffffu : 0) | (keep(off + 3) ? 0xffff0000u : 0);
-#pragma unroll
-                                    for (int db = 0; db < DB; ++db) {
-                                        vf[b][t * DB + db][2 * g] &= m0;
-                                        vf[b][t * DB + db][2 * g + 1] &= m1;
-                                    }
-                                }
-                            }
-                    }
-                }
-            }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[b][r]);
-            mx = fmaxf(m, pair_max(mx) * a.scale_log2);      // scale > 0
-            const float ref = finite_or_0(mx);
-            if (step > 0) {
-                const float alpha = exp2_flush(m - ref);
-                l *= alpha;
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
-            }
-            m = mx;
+                for (int r = 0; r < 16; ++r) sacc[b][r] = add_eighth(sacc[b][r]);
+        // lane (column lq, half lh) holds positions w0 + 32 b + 8 (r / 4) + 4 lh + r % 4
+        if (w0 + 63 > p_min || (a.window && w0 <= p_max - a.window) || !whole) {
+            const int from = first_seen(qpos, a.window);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float p = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
-                    sacc[b][r] = p;
-                    l += p;
+                    const int pos = w0 + b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+                    const uint32_t reach = id[b] >= 0 ? qpos - from + 1 : 0;
+                    sacc[b][r] = (uint32_t)(pos - from) < reach ? sacc[b][r] : -INFINITY;
+                    __builtin_amdgcn_sched_barrier(0);   // one at a time: 32 lane masks do not fit the scalar registers
                 }
+            if (w0 + 64 > hi || w0 < lo || !whole) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t length = id[b] >= 0 ? hi - lo : 0;
+                    auto keep = [&](int off) { return (uint32_t)(w0 + 32 * b + 4 * lh + off - lo) < length; };   // inside the block
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    bf16x8 pf;
+                    for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) pf[x] = (bf16)sacc[b][8 * t + x];
+                        for (int g = 0; g < 2; ++g) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const int off = 16 * t + 8 * g;      // positions 16 t + 8 g + 4 lh + 0..3
+                            if (E4M3) {
+                                const uint32_t k4 = (keep(off) ? 0xffu : 0) | (keep(off + 1) ? 0xff00u : 0) |
+                                                    (keep(off + 2) ? 0xff0000u : 0) | (keep(off + 3) ? 0xff000000u : 0);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        bf16x8 vv;
-                        if (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
-                        else vv = *reinterpret_cast<const bf16x8*>(&vf[b][t * DB + db]);
-                        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
-                    }
+                                for (int x = 0; x < NF; ++x) vf[b][x][2 * t + g] &= k4;
+                            } else {
+                                const uint32_t m0 = (keep(off) ? 0xffffu : 0) | (keep(off + 1) ? 0xffff0000u : 0);
+                                const uint32_t m1 = (keep(off + 2) ? 0xffffu : 0) | (keep(off + 3) ? 0xffff0000u : 0);
+#pragma unroll
+                                for (int db = 0; db < DB; ++db) {
+                                    vf[b][t * DB + db][2 * g] &= m0;
+                                    vf[b][t * DB + db][2 * g + 1] &= m1;
+                                }
+                            }
+                        }
                 }
-            if (step + 1 < STEPS && begin(step + 1) < hi) load_v(step + 1);
+            }
         }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[b][r]);
+        m = pair_max(mx) * a.scale_log2;                 // scale > 0
+        const float ref = finite_or_0(m);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
+                sacc[b][r] = p;
+                l += p;
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                bf16x8 pf;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) pf[x] = (bf16)sacc[b][8 * t + x];
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    bf16x8 vv;
+                    if (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
+                    else vv = *reinterpret_cast<const bf16x8*>(&vf[b][t * DB + db]);
+                    oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
+                }
+            }
         l = pair_sum(l);
     }
     // a wave that had nothing leaves m = -inf, l = 0, o = 0
@@ -452,8 +451,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_narrow_join_kernel(PagedQu
     const int s = bv.decode_seqs[i];
     const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
     if (token >= n || h >= a.Hq) return;
-    const int ch = kDecodeChunk * w.steps;
-    int nch = (before + n - (first_seen(before, a.window) & ~63) + ch - 1) / ch;
+    int nch = (before + n - (first_seen(before, a.window) & ~63) + kDecodeChunk - 1) / kDecodeChunk;
     if (nch == 1) return;                                    // the output is there
     if (nch > w.max_chunks) nch = w.max_chunks;
     const size_t at = partial_at(w, bv.n_decode, i, token, a.Hq, h, 0);
@@ -850,12 +848,9 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
     if (n_narrow > 0) {
         // waves per SIMD: what the registers, and with 32 rows the LDS, leave room for; two for bf16 of d = 128, where a third
         // keeps the memory streams in shorter runs
-        constexpr int FEW = E4M3 ? (D == 128 ? 3 : 4) : D == 128 ? 2 : 4;
+        constexpr int FEW = E4M3 || D == 64 ? 4 : 2;
         const unsigned grid = (unsigned)((w.list + (n_narrow - w.first) * w.chunks) * kv.Hkv * w.col_tiles);
-        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, 1, FEW> : paged_narrow_kernel<D, E4M3, kNarrowRows, 1, 3>;
-        if constexpr (E4M3)                                  // bf16 takes one step always
-            if (w.steps == 2)
-                kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, 2, D == 128 ? 3 : 4> : paged_narrow_kernel<D, E4M3, kNarrowRows, 2, 3>;
+        auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, FEW> : paged_narrow_kernel<D, E4M3, kNarrowRows, 3>;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
         if (w.max_chunks > 1) {
             const unsigned tokens = (unsigned)(bv.n_decode + w.n_short * w.short_tokens);

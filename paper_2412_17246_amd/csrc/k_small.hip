@@ -474,11 +474,11 @@ void launch_kv_scatter(const act_t* src_k, const act_t* src_v, const KvView& kv,
 __global__ __launch_bounds__(256) void batch_advance_kernel(int32_t* kv_before, int B, const int32_t* __restrict__ decode_seqs,
                                                             const int32_t* __restrict__ seq_slot, int n_decode, int4* work,
                                                             int capacity) {
-    __shared__ int scan[256], scan2[256];                    // entries, and pairs of them
-    __shared__ int base, base2;
+    __shared__ int scan[256];
+    __shared__ int base;
     const int tid = threadIdx.x;
     for (int i = tid; i < B; i += 256) kv_before[i] += 1;
-    if (tid == 0) base = base2 = 0;
+    if (tid == 0) base = 0;
     __syncthreads();
     for (int d0 = 0; d0 < n_decode; d0 += 256) {
         const int di = d0 + tid;
@@ -487,36 +487,25 @@ __global__ __launch_bounds__(256) void batch_advance_kernel(int32_t* kv_before, 
             s = decode_seqs[di];
             n = (kv_before[s] + 1 + kDecodeChunk - 1) / kDecodeChunk;
         }
-        const int n2 = (n + 1) / 2;
         scan[tid] = n;
-        scan2[tid] = n2;
         __syncthreads();
         for (int step = 1; step < 256; step <<= 1) {
-            const int add = tid >= step ? scan[tid - step] : 0, add2 = tid >= step ? scan2[tid - step] : 0;
+            const int add = tid >= step ? scan[tid - step] : 0;
             __syncthreads();
             scan[tid] += add;
-            scan2[tid] += add2;
             __syncthreads();
         }
-        const int at = base + scan[tid] - n, at2 = base2 + scan2[tid] - n2;
+        const int at = base + scan[tid] - n;
         if (n > 0) {
             const int slot = seq_slot[s];
             for (int c = 0; c < n; ++c)
                 if (at + c < capacity) {
                     work[2 * (at + c)] = make_int4(s, slot, di, n);
-                    work[2 * (at + c) + 1].x = at;
-                }
-            for (int c = 0; c < n2; ++c)
-                if (at2 + c < capacity) {
-                    work[2 * (at2 + c) + 1].y = di;
-                    work[2 * (at2 + c) + 1].z = at2;
+                    work[2 * (at + c) + 1] = make_int4(at, 0, 0, 0);
                 }
         }
         __syncthreads();
-        if (tid == 255) {
-            base += scan[255];
-            base2 += scan2[255];
-        }
+        if (tid == 255) base += scan[255];
         __syncthreads();
     }
 }

@@ -114,12 +114,11 @@ inline Divisor divisor(int d) {
 
 // How the attention of a batch is cut, from the host's copy of its lengths.  A sequence's new tokens times the query heads of a
 // kv head are its rows there.  Narrow: single new tokens, and sequences of few rows; a workgroup takes up to kNarrowRows of them
-// over one chunk of kDecodeChunk positions, or of twice as many (`steps`).  Wide: a workgroup takes kWideRows rows over the keys they see, or over one of
+// over one chunk of kDecodeChunk positions.  Wide: a workgroup takes kWideRows rows over the keys they see, or over one of
 // `splits` ranges of them.
 constexpr int kNarrowRows = 32, kWideRows = 128;
 struct PagedWork {
     int n_short, short_tokens; // sequences of several tokens that are narrow (the first of BatchView::short_seqs), their most tokens
-    int steps;
     int list;                  // workgroups of single tokens that the batch's work list names (no window), for one kv head
     int first;                 // sequences of decode_seqs and short_seqs from here on have `chunks` workgroups each per kv head
     int chunks;

@@ -65,7 +65,7 @@ int lengths_ok(const bz_batch* b, const bz_paged_kv* kv, const float* rope, int 
     return BZ_OK;
 }
 
-int64_t chunks_of(int64_t keys, int steps) { return (keys + (int64_t)kDecodeChunk * steps - 1) / (kDecodeChunk * steps); }
+int chunks_of(int64_t keys) { return (int)((keys + kDecodeChunk - 1) / kDecodeChunk); }
 
 // keys that the tokens of a sequence see between them, from a multiple of 64 on
 int64_t keys_of(int64_t before, int64_t n, int window) {
@@ -73,7 +73,7 @@ int64_t keys_of(int64_t before, int64_t n, int window) {
     return before + n - lo;
 }
 
-PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int window, bool e4m3) {
+PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int window) {
     PagedWork w{};
     const int G = Hq / Hkv;
     int64_t most = 0;
@@ -81,30 +81,14 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
     while (w.n_short < (int)b->short_qlen.size() && b->short_qlen[w.n_short] * G <= kNarrowRows) ++w.n_short;
     w.short_tokens = w.n_short ? b->short_qlen[w.n_short - 1] : 0;
     for (int i = 0; i < w.n_short; ++i) most = std::max(most, keys_of(b->kv_before[b->short_seqs[i]], b->short_qlen[i], window));
-    int64_t longest = 0;                                     // of the single tokens' caches
-    for (int s : b->decode_seqs) {
-        longest = std::max<int64_t>(longest, (int64_t)b->kv_before[s] + 1);
-        if (window) most = std::max(most, keys_of(b->kv_before[s], 1, window));
-    }
+    if (window)
+        for (int s : b->decode_seqs) most = std::max(most, keys_of(b->kv_before[s], 1, window));
     w.col_tiles = (std::max(G, 1) + kNarrowRows - 1) / kNarrowRows;
     w.narrow_rows = std::max(std::min(G, kNarrowRows), w.short_tokens * G);
+    w.list = window ? 0 : bv.n_decode_work;
     w.first = window ? 0 : bv.n_decode;
-    // e4m3: chunks of two steps, where half as many workgroups still fill the chip
-    auto cut = [&](int steps) {
-        int64_t list = 0;
-        if (!window)
-            for (int s : b->decode_seqs) list += chunks_of((int64_t)b->kv_before[s] + 1, steps);
-        w.steps = steps;
-        w.list = (int)list;
-        w.chunks = (int)chunks_of(most, steps);
-        w.max_chunks = (int)std::max<int64_t>(w.chunks, window ? 0 : chunks_of(longest, steps));
-        int64_t n = list;                                    // workgroups that have work, for one kv head
-        for (int i = 0; i < w.n_short; ++i) n += chunks_of(keys_of(b->kv_before[b->short_seqs[i]], b->short_qlen[i], window), steps);
-        if (window)
-            for (int s : b->decode_seqs) n += chunks_of(keys_of(b->kv_before[s], 1, window), steps);
-        return n * Hkv * w.col_tiles;
-    };
-    if (!e4m3 || cut(2) < 512) cut(1);
+    w.chunks = chunks_of(most);
+    w.max_chunks = std::max(w.chunks, window ? 0 : bv.decode_chunks);
     int64_t units = 0, keys = 0;
     for (int s = 0; s < b->B; ++s) {
         const int n = b->q_start[s + 1] - b->q_start[s];
@@ -180,7 +164,7 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
 size_t bz_op_paged_attention_workspace_bytes(const bz_batch* batch, const bz_paged_kv* kv, int n_q_heads, int window) {
     if (!batch || !shape_ok(kv) || n_q_heads < 1 || n_q_heads % kv->n_kv_heads || n_q_heads > 1024 || window < 0) return 0;
     const BatchView bv = batch_view(batch);
-    return paged_attention_bytes(work_of(batch, bv, n_q_heads, kv->n_kv_heads, window, kv->dtype == BZ_KV_E4M3), bv, n_q_heads, kv->n_kv_heads, kv->head_dim);
+    return paged_attention_bytes(work_of(batch, bv, n_q_heads, kv->n_kv_heads, window), bv, n_q_heads, kv->n_kv_heads, kv->head_dim);
 }
 
 int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const void* q, int64_t q_stride, void* out,
@@ -196,7 +180,7 @@ int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const vo
     int rc = lengths_ok(batch, kv, rope, rope_positions);
     if (rc) return rc;
     const BatchView bv = batch_view(batch);
-    const PagedWork work = work_of(batch, bv, n_q_heads, kv->n_kv_heads, window, kv->dtype == BZ_KV_E4M3);
+    const PagedWork work = work_of(batch, bv, n_q_heads, kv->n_kv_heads, window);
     const size_t need = paged_attention_bytes(work, bv, n_q_heads, kv->n_kv_heads, kv->head_dim);
     if (need && (!workspace || workspace_bytes < need)) return BZ_ENOMEM;
     rc = batch_before_run(batch, st);

@@ -62,7 +62,7 @@ def test_page_sizes(torch, e4m3, page):
 @CACHES
 @pytest.mark.parametrize("window", [0, 200])
 def test_many_sequences(torch, e4m3, window):
-    """Enough workgroups for chunks of two steps in e4m3, odd and even numbers of chunks, one chunk among them."""
+    """Odd and even numbers of chunks, one chunk among them, ends on either side of a chunk's."""
     rng = np.random.default_rng(24)
     seqs = [(1, int(n)) for n in rng.integers(0, 1300, 90)] + [(2, 511), (3, 513), (1, 255), (1, 256), (1, 511), (1, 512)]
     w = World(torch, seqs, 8, 8, 64, 64, e4m3=e4m3, seed=24)
@@ -72,7 +72,7 @@ def test_many_sequences(torch, e4m3, window):
 
 @CACHES
 def test_decode_steps_of_an_advanced_batch(torch, e4m3):
-    """A batch of single tokens advanced on the device: its chunks, pairs of chunks and lengths grow, pages fill."""
+    """A batch of single tokens advanced on the device: its chunks and lengths grow, pages fill."""
     from paper_2412_17246_amd import Instance
     import workloads as W
     steps, rng = 6, np.random.default_rng(25)
