@@ -500,19 +500,23 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
 
 /* Attention of the batch's new tokens over the pages, which hold them already (bz_op_paged_append comes first): query head h of
  * the token at position p reads kv head h / (n_q_heads / n_kv_heads) at positions 0..p, with window > 0 only at the last `window`
- * of them, p itself included.  Scores are multiplied by `scale` (positive and finite; 0: 1/sqrt(head_dim)).  q and out hold
- * n_q_heads * head_dim activation elements per packed row, rows q_stride and out_stride elements apart (multiples of 8; pointers
- * 16-byte aligned); they may be the same memory only if strides agree as well.  `rope`: as above, queries are rotated as they are
- * read; NULL: they are rotated already, or there is no rotation.  A query that sees no position gets zeros.  Sequences without new tokens and rows of out
- * behind the last sequence are left alone.  Softmax and sums are float; weights are rounded to bf16 for the product with the values.
+ * of them, p itself included.  Scores are multiplied by `scale` (positive and finite; 0: 1/sqrt(head_dim)).  A query that sees no
+ * position gets zeros.
+ * q and out hold n_q_heads * head_dim activation elements per packed row, rows q_stride and out_stride elements apart (multiples of
+ * 8; pointers 16-byte aligned); out may be q itself, with the same stride.  Rows of out behind the last sequence are left alone.
+ * `rope`: as above, queries are rotated as they are read; NULL: they are rotated already, or there is no rotation.
+ * Softmax and sums are float.  Rounded to bf16 (not in the fp32 debug build) are the weights, for the product with the values, and
+ * a rotated query, for the product with the keys: to one bf16, or, in sequences whose new tokens times n_q_heads / n_kv_heads are
+ * at most 32 and of single tokens always, to two whose sum it is.
  * A value that is not finite shows in every query that sees it, and may show in queries of the same sequence and call that come
- * before it.  `workspace`: device scratch, 16-byte aligned, of at least bz_op_paged_attention_workspace_bytes() bytes for the same
- * batch, shapes and window (BZ_ENOMEM if smaller); calls that may overlap in time need workspaces of their own.
+ * before it; in no other sequence.
+ * `workspace`: device scratch, 16-byte aligned, of at least bz_op_paged_attention_workspace_bytes() bytes for the same batch,
+ * shapes and window (BZ_ENOMEM if smaller); calls that may overlap in time need workspaces of their own.
  * Results depend within rounding on the other sequences of the batch, whose lengths say how key ranges are cut; the same call
  * gives the same bits every time.
  *
- * The stream of an append or an attention has to exist until the batch is next rebuilt, advanced or destroyed: that is when the
- * library orders a change behind what was enqueued there.
+ * A batch is used from one host thread at a time.  The stream of an append or an attention has to exist until the batch is next
+ * rebuilt, advanced or destroyed: that is when the library orders a change behind what was enqueued there.
  *
  * Both operations may be captured into a graph.  It replays the batch as it was: rebuilding, advancing or destroying the batch
  * means capturing again, and is not ordered behind replays by the library.  Under capture a batch that was last rebuilt or

@@ -695,6 +695,13 @@ def _rows(kv: PagedKv, batch: Batch, x, what: str) -> int:
     return shape[1]
 
 
+def _on_device(kv: PagedKv) -> None:
+    """Operations run on the current device: memory of another is refused."""
+    import torch
+    if torch.cuda.current_device() != kv._device.index:
+        raise ValueError(f"the cache is on {kv._device}, which is not the current device")
+
+
 def _pitch(x) -> int:
     """Elements from a row to the next (torch may say anything where there is only one)."""
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
@@ -711,6 +718,7 @@ def _rope(kv: PagedKv, rope):
 def op_paged_append(batch: Batch, kv: PagedKv, k, v, rope=None, stream=None) -> None:
     """Appends the batch's keys (rotated on the way with `rope`) and values, [T, n_kv_heads * head_dim] each, to the pages;
     both may be columns of one wider tensor."""
+    _on_device(kv)
     width = kv.n_kv_heads * kv.head_dim
     if _rows(kv, batch, k, "k") != width or _rows(kv, batch, v, "v") != width:
         raise ValueError("a row of k and v must be n_kv_heads * head_dim elements")
@@ -728,6 +736,7 @@ def op_paged_attention_workspace_bytes(batch: Batch, kv: PagedKv, n_q_heads: int
 def op_paged_attention(batch: Batch, kv: PagedKv, q, out, scale: float = 0.0, window: int = 0, rope=None, workspace=None,
                        stream=None) -> None:
     """Attention of the batch's new tokens, which the pages hold already, for q [T, n_q_heads * head_dim] into `out`."""
+    _on_device(kv)
     width = _rows(kv, batch, q, "q")
     if _rows(kv, batch, out, "out") != width or width % kv.head_dim:
         raise ValueError("a row of q and out must be n_q_heads * head_dim elements")
@@ -743,6 +752,7 @@ def op_paged_attention(batch: Batch, kv: PagedKv, q, out, scale: float = 0.0, wi
 
 def op_paged_read(kv: PagedKv, row: int, pos0: int, n: int, k, v, stream=None) -> None:
     """Positions pos0 .. pos0 + n - 1 of a table row into k and v, contiguous [n, n_kv_heads, head_dim]."""
+    _on_device(kv)
     need = n * kv.n_kv_heads * kv.head_dim
     for x in (k, v):
         if x.dtype != kv._act or x.device != kv._device or not x.is_contiguous() or x.numel() < need:

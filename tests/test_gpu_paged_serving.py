@@ -125,6 +125,15 @@ def test_rebuilt_batches_on_two_streams(torch):
     batch.close()
 
 
+@CACHES
+def test_output_in_place_of_the_queries(torch, e4m3):
+    w = World(torch, [(1, 700), (200, 150), (4, 600), (33, 2000), (1, 20)], 8, 2, 128, 64, e4m3=e4m3, seed=43)
+    w.write_new()
+    w.q = w.q.contiguous()
+    want = w.attend()
+    assert torch.equal(w.attend(out=w.q), want)
+
+
 def test_two_streams_at_once(torch):
     """Two calls in flight, with a workspace each; a batch of its own each, and one for both."""
     import paper_2412_17246_amd as lib
