@@ -161,7 +161,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     constexpr int NF = E4M3 ? D / 32 : D / 16;               // 16-byte loads per lane and block, of K and again of V
     __shared__ float wmx[4][RT], wsum[4][RT];
     constexpr int PARTS = RT > 8 ? 2 : 1, DP = D / PARTS;    // of the head dim that are merged at a time: LDS for one workgroup more
-    __shared__ float osh[4][RT][DP];
+    __shared__ __attribute__((aligned(16))) float osh[4][RT][DP + 4];        // rows 16 bytes out of step: lanes write rows
     __shared__ __attribute__((aligned(16))) bf16 qs[2][RT][LD];
 
     const int G = w.by_group.d;

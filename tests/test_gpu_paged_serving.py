@@ -301,3 +301,52 @@ def test_refusals(torch):
             bad()
     with pytest.raises(lib.BzError):
         lib.PagedKv(16, 2, 128, k=w.dk, v=w.dv, page_table=w.dtable)
+
+
+def test_a_layer_by_single_operations_agrees_with_run_layers(torch):
+    """Two steps of one decoder layer, a prompt with a chunk beside it and then a token each: norm, projections and SwiGLU by the single
+    operations around the paged cache, against the oracle and beside bz_run_layers on its own cache."""
+    import paper_2412_17246_amd as lib
+    import workloads as W
+    from oracle import decoder as O
+    from tests import _util as U
+    s = W.CONFIGS["tiny"]
+    bits = W.layer_weights_bits(s, 0)
+    inst = U.make_instance(s, max_seqs=2, max_seq_len=256, max_tokens=128, kv_tokens=512)
+    pinned = inst.pinned_blob(inst.pack_layer(bits))
+    inst.load_layer(0, pinned)
+    for slot in range(2):
+        inst.kv_reserve(slot, 256)
+    blob = pinned.cuda()
+    at = lambda name, rows, cols: blob[getattr(inst.layout, name):][:rows * cols * 2].view(torch.bfloat16)  # noqa: E731
+    Hq, Hkv, d, H, F = s.Hq, s.Hkv, s.d, s.H, s.F
+    nqkv = (Hq + 2 * Hkv) * d
+    table = torch.tensor([[3, 0, 5, 1], [2, 4, 7, 6]], dtype=torch.int32, device="cuda")
+    k, v = (torch.full((8, Hkv, 64 * d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    kv = lib.PagedKv(64, Hkv, d, k=k, v=v, page_table=table)
+    rope = torch.from_numpy(lib.rope_table(256, d, s.rope_base)).cuda()
+    osh, wts, okv = U.oracle_shape(s), {0: U.oracle_weights(bits)}, O.OracleKV()
+    for step, (q_start, before) in enumerate([([0, 70, 90], [0, 0]), ([0, 1, 2], [70, 20])]):
+        T = q_start[-1]
+        xbits = W.bf16_bits_from_f32((np.random.default_rng([61, step]).standard_normal((T, H)) / 16).astype(np.float32))
+        x = U.to_device(xbits, False)
+        y = x.clone()
+        batch = lib.Batch(lib.load_library(), q_start, [0, 1], before)
+        normed, qkv = torch.empty_like(x), torch.empty(T, nqkv, dtype=torch.bfloat16, device="cuda")
+        attn, act = (torch.empty(T, n, dtype=torch.bfloat16, device="cuda") for n in (Hq * d, F))
+        ws = torch.empty(max(16, lib.op_paged_attention_workspace_bytes(batch, kv, Hq)), dtype=torch.uint8, device="cuda")
+        lib.op_rmsnorm(x, at("g1", 1, H), normed, s.eps)
+        lib.op_gemm(0, normed, at("wq", nqkv, H), None, qkv, T, nqkv, H)
+        lib.op_paged_append(batch, kv, qkv[:, Hq * d:(Hq + Hkv) * d], qkv[:, (Hq + Hkv) * d:], rope=rope)
+        lib.op_paged_attention(batch, kv, qkv[:, :Hq * d], attn, rope=rope, workspace=ws)
+        lib.op_gemm(1, attn, at("wo", H, Hq * d), x, x, T, H, Hq * d)
+        lib.op_rmsnorm(x, at("g2", 1, H), normed, s.eps)
+        lib.op_gemm(2, normed, at("wg", 2 * F, H), None, act, T, F, H)
+        lib.op_gemm(1, act, at("wd", H, F), x, x, T, H, F)
+        inst.run_layers(0, 1, batch, y)
+        inst.sync()
+        want = O.run_layers(osh, wts, 0, 1, U.f64(xbits), O.OracleBatch(q_start, [0, 1], before), okv)
+        for got in (x, y):
+            assert U.rel_err(U.from_device(got), want) <= U.BF16_TOL
+            U.assert_rms(U.from_device(got), want, U.RMS_BF16)
+    inst.close()
