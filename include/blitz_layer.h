@@ -500,14 +500,15 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
 
 /* Attention of the batch's new tokens over the pages, which hold them already (bz_op_paged_append comes first): query head h of
  * the token at position p reads kv head h / (n_q_heads / n_kv_heads) at positions 0..p, with window > 0 only at the last `window`
- * of them, p itself included.  Scores are multiplied by `scale` (positive and finite; 0: 1/sqrt(head_dim)).  A query that sees no
- * position gets zeros.
+ * of them, p itself included.  Scores are multiplied by `scale` (positive; 0: 1/sqrt(head_dim)), whose product with k_scale and
+ * log2 e has to be a normal float, neither infinite nor denormal.  A query that sees no position gets zeros.
  * q and out hold n_q_heads * head_dim activation elements per packed row, rows q_stride and out_stride elements apart (multiples of
  * 8; pointers 16-byte aligned); out may be q itself, with the same stride.  Rows of out behind the last sequence are left alone.
  * `rope`: as above, queries are rotated as they are read; NULL: they are rotated already, or there is no rotation.
- * Softmax and sums are float.  Rounded to bf16 (not in the fp32 debug build) are the weights, for the product with the values, and
- * a rotated query, for the product with the keys: to one bf16, or, in sequences whose new tokens times n_q_heads / n_kv_heads are
- * at most 32 and of single tokens always, to two whose sum it is.
+ * Softmax and sums are float.  Rounded (not in the fp32 debug build) are the weights, to bf16 for the product with the values, and a
+ * rotated query, for the product with the keys, to two bf16 whose sum it is.  Over BZ_KV_E4M3, in sequences whose new tokens times
+ * n_q_heads / n_kv_heads exceed 32, weights and queries are fp16 instead: 11 bits, and elements of a query below 2^-38 of its
+ * largest count as nothing.
  * A value that is not finite shows in every query that sees it, and may show in queries of the same sequence and call that come
  * before it; in no other sequence.
  * `workspace`: device scratch, 16-byte aligned, of at least bz_op_paged_attention_workspace_bytes() bytes for the same batch,

@@ -10,6 +10,8 @@
 // (behind the sequence, before the window, on a page that is not there) are cleared before the product.
 #include "paged.h"
 
+#include <cfloat>
+
 namespace bz {
 
 #ifndef BZ_FP32_DEBUG
@@ -17,6 +19,8 @@ namespace {
 
 typedef __attribute__((address_space(3))) void* lptr_t;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // weights below the normal range flush to zero: the largest of a row's is 1
 __device__ __forceinline__ float exp2_flush(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -31,21 +35,57 @@ __device__ __forceinline__ bf16x8 e4m3_to_bf16(uint32_t a, uint32_t b) {
     return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
-// 8 pairs (j0 + e, j0 + e + d/2) of a query: as they are, or rotated, scaled and rounded to bf16 once
-template <bool ROTATE>
-__device__ __forceinline__ void query8(const bf16* q, const float* cs, float scale, int half, bf16x8& lo8, bf16x8& hi8) {
-    lo8 = *reinterpret_cast<const bf16x8*>(q);
-    hi8 = *reinterpret_cast<const bf16x8*>(q + half);
+// eight e4m3 numbers to fp16, which holds each of them exactly as well
+__device__ __forceinline__ f16x8 e4m3_to_f16(uint32_t a, uint32_t b) {
+    const f16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+    const f16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+    return f16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+
+__device__ __forceinline__ f32x16 product(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 product(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+// c plus the sum of a pair of weights
+__device__ __forceinline__ float add_pair(bf16x2 p, float c) { return __builtin_amdgcn_fdot2_f32_bf16(p, bf16x2{(bf16)1.f, (bf16)1.f}, c, false); }
+__device__ __forceinline__ float add_pair(f16x2 p, float c) { return __builtin_amdgcn_fdot2(p, f16x2{(_Float16)1.f, (_Float16)1.f}, c, false); }
+
+// 8 pairs (j0 + e, j0 + e + d/2) of a query: as they are, or rotated and scaled, as the sum of two bf16
+template <bool ROTATE, int QP>
+__device__ __forceinline__ void query8(const bf16* q, const float* cs, float scale, int half, bf16x8 (&lower)[QP], bf16x8 (&upper)[QP]) {
+    lower[0] = *reinterpret_cast<const bf16x8*>(q);
+    upper[0] = *reinterpret_cast<const bf16x8*>(q + half);
     if (!ROTATE) return;
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        const float4 v = *reinterpret_cast<const float4*>(cs + 2 * e);
-        const float l0 = (float)lo8[e], h0 = (float)hi8[e], l1 = (float)lo8[e + 1], h1 = (float)hi8[e + 1];
-        lo8[e] = (bf16)((l0 * v.x - h0 * v.y) * scale);
-        hi8[e] = (bf16)((h0 * v.x + l0 * v.y) * scale);
-        lo8[e + 1] = (bf16)((l1 * v.z - h1 * v.w) * scale);
-        hi8[e + 1] = (bf16)((h1 * v.z + l1 * v.w) * scale);
+    for (int e = 0; e < 8; ++e) {
+        const float2 v = *reinterpret_cast<const float2*>(cs + 2 * e);
+        const float y = (float)lower[0][e], z = (float)upper[0][e];
+        const float a = (y * v.x - z * v.y) * scale, b = (z * v.x + y * v.y) * scale;
+        lower[0][e] = (bf16)a;
+        upper[0][e] = (bf16)b;
+        lower[QP - 1][e] = (bf16)(a - (float)lower[0][e]);
+        upper[QP - 1][e] = (bf16)(b - (float)upper[0][e]);
     }
+}
+
+// the same in fp16, times `factor`, which keeps the row within range
+template <bool ROTATE>
+__device__ __forceinline__ void query8(bf16x8 y8, bf16x8 z8, const float* cs, float factor, f16x8& lower, f16x8& upper) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float2 v = ROTATE ? *reinterpret_cast<const float2*>(cs + 2 * e) : make_float2(1.f, 0.f);
+        const float y = (float)y8[e] * factor, z = (float)z8[e] * factor;
+        lower[e] = (_Float16)(ROTATE ? y * v.x - z * v.y : y);
+        upper[e] = (_Float16)(ROTATE ? z * v.x + y * v.y : z);
+    }
+}
+// largest exponent of eight numbers, as bf16 holds it
+__device__ __forceinline__ int top_exponent(bf16x8 v, int top) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bf16 x = v[e];
+        const int m = (__builtin_bit_cast(uint16_t, x) >> 7) & 255;
+        top = m > top ? m : top;
+    }
+    return top;
 }
 
 // the larger, or the sum, of a lane's value and that of its partner 32 lanes on: a vector instruction, no trip through LDS
@@ -68,7 +108,7 @@ __device__ __forceinline__ float pair_sum(float x) {
 // largest score so far: then most tiles leave the accumulators alone.  Weights are at most 2^kLag, and the row's largest at
 // least 1 when the reference was set; everything is relative to it and no bits are lost.
 constexpr float kLag = 8.f;
-template <int DB, bool SCALED>
+template <int DB, bool SCALED, typename P2, typename P8, int TOP>
 struct RowSoftmax {
     float ref = 0.f, l = 0.f;            // l over this lane's half of the keys
     bool seen = false;                   // the reference is one
@@ -78,17 +118,17 @@ struct RowSoftmax {
 #pragma unroll
         for (int x = 0; x < 16; ++x) start[x] = 0.f;
     }
-    // scores (SCALED: in base 2, the reference taken off by the product; else raw) to weights in bf16
-    __device__ __forceinline__ void weigh(f32x16 (&s)[2], float scale, f32x16 (&o)[DB], bf16x8 (&pf)[4]) {
+    // scores (SCALED: in base 2, the reference taken off by the product; else raw) to weights
+    __device__ __forceinline__ void weigh(f32x16 (&s)[2], float scale, f32x16 (&o)[DB], P8 (&pf)[4]) {
         float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[kb][x]);
         mx = SCALED ? pair_max(mx) : fmaf(pair_max(mx), scale, -ref);      // above the reference
-        const bool move = mx > (seen ? kLag : -INFINITY);
+        const bool move = mx > (seen ? TOP + kLag : -INFINITY);
         if (__builtin_amdgcn_ballot_w64(move) != 0) {
-            const float up = move ? mx : 0.f, alpha = move && !seen ? 0.f : exp2_flush(-up);
+            const float up = move ? mx - TOP : 0.f, alpha = move && !seen ? 0.f : exp2_flush(-up);
             seen |= move;
             ref += up;
             l *= alpha;
@@ -105,14 +145,15 @@ struct RowSoftmax {
                 for (int x = 0; x < 16; ++x) start[x] = -ref;
             }
         }
-        const bf16x2 ones = {(bf16)1.f, (bf16)1.f};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
                 const float a = s[t >> 1][8 * (t & 1) + e], b = s[t >> 1][8 * (t & 1) + e + 1];
-                const bf16x2 p = {(bf16)exp2_flush(SCALED ? a : fmaf(a, scale, -ref)), (bf16)exp2_flush(SCALED ? b : fmaf(b, scale, -ref))};
-                l = __builtin_amdgcn_fdot2_f32_bf16(p, ones, l, false);    // the sum of the weights as the product will use them
+                P2 p;
+                p[0] = exp2_flush(SCALED ? a : fmaf(a, scale, -ref));
+                p[1] = exp2_flush(SCALED ? b : fmaf(b, scale, -ref));
+                l = add_pair(p, l);                          // the sum of the weights as the product will use them
                 pf[t][e] = p[0];
                 pf[t][e + 1] = p[1];
             }
@@ -493,8 +534,19 @@ __global__ __launch_bounds__(kJoinThreads) void paged_narrow_join_kernel(PagedQu
 // Wide: 128 rows per workgroup, 32 per wave, keys in tiles of 64 through LDS.  S^T = K Q^T, so that a lane pair (lane, lane + 32)
 // owns a row: its maximum and sum need one exchange, the rescale of O^T is a per-lane factor, and P^T goes from the score
 // accumulators into O^T = V^T P^T without leaving registers, since V's pieces hold the positions in the accumulators' order.
-// Activation caches move global -> LDS by DMA, the next tile's loads between the score products; e4m3 goes through registers, where it
-// becomes bf16, one tile ahead.  Bound by the vector pipe (32 exponentials per lane and tile) and the matrix pipe.
+// Activation caches move global -> LDS by DMA, the next tile's loads between the score products; e4m3 goes through registers, one tile
+// ahead, where it becomes fp16.
+//
+// What is rounded: a bf16 cache is multiplied by queries that are, after the rotation, the sum of two bf16, and by weights in bf16;
+// an e4m3 cache, which fp16 holds exactly, by queries and weights in fp16, a query's row brought to fp16's range by a power of two
+// that its scores give back.  Distance of the output from a computation in 64 bits, rms: 2.0e-3 to 2.3e-3 over bf16 and 1.7e-3, the
+// output's own rounding, over e4m3.  With rotated queries in one bf16 it is 2.5e-3 to 2.9e-3, and the 48 products per tile and wave are
+// 32 (four prompts of 2048 tokens on 8 kv heads with eight query heads each: 305 us, with two 381).
+//
+// Bound by the matrix pipe: those 48 products of random numbers take 1.2 us at the clock that the chip's power allows (25 ns each and
+// SIMD, registers only), a tile 1.3.  The softmax between them is the other wave's time on the SIMD: 32 exponentials, 16 of each of
+// maximum, conversion and sum.  Its pieces that pay: a reference that lags the maximum (above), taken off by the product
+// itself, which starts from it; the tile's sum as a product with ones.
 // ---------------------------------------------------------------------------------------------
 struct WideUnit {
     int item, sub, split, kvh;
@@ -578,6 +630,9 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     constexpr int NL = D / 32;           // 1 KiB DMA loads per wave and tile, of K and again of V
     constexpr int NC = D / 64;           // e4m3: 16-byte loads per thread and tile, of K and again of V
     constexpr int STAGE = 4 * BLK;       // K tile (two blocks), V tile (two blocks)
+    // two bytes each: the cache's bf16, or e4m3 as fp16
+    using T2 = typename std::conditional<E4M3, f16x2, bf16x2>::type;
+    using T8 = typename std::conditional<E4M3, f16x8, bf16x8>::type;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     bf16* smem = reinterpret_cast<bf16*>(smem_raw);
 
@@ -633,10 +688,10 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         for (int i = 0; i < NC; ++i) {
             const int c = tid + 256 * i, blk = NC == 2 ? i : wblk, in = c - blk * (2 * D);
             const int piece = in >> 5, p = in & 31, h = in / D, j = in - h * D;
-            *reinterpret_cast<bf16x8*>(ks + blk * BLK + ((2 * piece) * 32 + p) * 8) = e4m3_to_bf16(kreg[i][0], kreg[i][1]);
-            *reinterpret_cast<bf16x8*>(ks + blk * BLK + ((2 * piece + 1) * 32 + p) * 8) = e4m3_to_bf16(kreg[i][2], kreg[i][3]);
-            *reinterpret_cast<bf16x8*>(vs + blk * BLK + (h * D + j) * 8) = e4m3_to_bf16(vreg[i][0], vreg[i][1]);
-            *reinterpret_cast<bf16x8*>(vs + blk * BLK + ((2 + h) * D + j) * 8) = e4m3_to_bf16(vreg[i][2], vreg[i][3]);
+            *reinterpret_cast<f16x8*>(ks + blk * BLK + ((2 * piece) * 32 + p) * 8) = e4m3_to_f16(kreg[i][0], kreg[i][1]);
+            *reinterpret_cast<f16x8*>(ks + blk * BLK + ((2 * piece + 1) * 32 + p) * 8) = e4m3_to_f16(kreg[i][2], kreg[i][3]);
+            *reinterpret_cast<f16x8*>(vs + blk * BLK + (h * D + j) * 8) = e4m3_to_f16(vreg[i][0], vreg[i][1]);
+            *reinterpret_cast<f16x8*>(vs + blk * BLK + ((2 + h) * D + j) * 8) = e4m3_to_f16(vreg[i][2], vreg[i][3]);
         }
     };
 
@@ -650,20 +705,40 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         for (int q = 0; q < 2 * NL; ++q) issue_one(src, 0, q);
     }
 
-    bf16x8 qf[KS];
+    constexpr int QP = !E4M3 && ROTATE ? 2 : 1;              // parts of a query: a rotated one does not fit one bf16
+    T8 qf[KS][QP];
+    float row_scale = a.scale_log2;      // of this lane's row, for raw scores
     {
-        const bf16* qp = a.q + (size_t)(q0 + token) * a.q_stride + head * D;
-        const float* cs = ROTATE ? rope_row(a.rope, qpos, D) : nullptr;
+        const bf16* qp = a.q + (size_t)(q0 + token) * a.q_stride + head * D + lh * 8;
+        const float* cs = ROTATE ? rope_row(a.rope, qpos, D) + 2 * (lh * 8) : nullptr;
+        if constexpr (E4M3) {
+            bf16x8 raw[KS];
+            int top = 0;
 #pragma unroll
-        for (int ks = 0; ks < KS / 2; ++ks)
-            query8<ROTATE>(qp + ks * 16 + lh * 8, cs + 2 * (ks * 16 + lh * 8), a.scale_log2, D / 2, qf[ks], qf[ks + KS / 2]);
+            for (int ks = 0; ks < KS; ++ks) {
+                raw[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+                top = top_exponent(raw[ks], top);
+            }
+            // to below 2^14 and, after the rotation, 2^15
+            top = (int)pair_max((float)top);
+            const int up = 140 - (top > 20 ? top : 20);
+            const float factor = ldexpf(1.f, up);
+            row_scale = fminf(fmaxf(ldexpf(a.scale_log2, -up), FLT_MIN), FLT_MAX);     // 0 times -inf, a masked score, is a NaN
+#pragma unroll
+            for (int ks = 0; ks < KS / 2; ++ks) query8<ROTATE>(raw[ks], raw[ks + KS / 2], cs + 32 * ks, factor, qf[ks][0], qf[ks + KS / 2][0]);
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < KS / 2; ++ks) query8<ROTATE>(qp + ks * 16, cs + 32 * ks, a.scale_log2, D / 2, qf[ks], qf[ks + KS / 2]);
+        }
     }
     f32x16 o[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int x = 0; x < 16; ++x) o[b][x] = 0.f;
-    RowSoftmax<DB, ROTATE> rows;         // queries that were rotated are scaled as well
+    // rotated queries that are the sum of two bf16 are scaled as well; fp16 has few exponents, its weights reach up to 2^(6 + kLag)
+    constexpr bool SCALED = QP == 2;
+    RowSoftmax<DB, SCALED, T2, T8, E4M3 ? 6 : 0> rows;
     rows.init();
 
     for (int tile = keys.t0; tile < keys.t1; ++tile) {
@@ -703,20 +778,21 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
         // operand fetch runs ahead of the products by hand: each K fragment of the first key block is replaced by the second
         // block's when its product has gone, and under the second block's the first V fragments are requested
         constexpr int EVERY = (2 * KS) / (2 * NL);
-        auto k_frag = [&](int kb, int ks) { return *reinterpret_cast<const bf16x8*>(&Ks[kb * BLK + ((ks * 2 + lh) * 32 + lq) * 8]); };
+        auto k_frag = [&](int kb, int ks) { return *reinterpret_cast<const T8*>(&Ks[kb * BLK + ((ks * 2 + lh) * 32 + lq) * 8]); };
         auto v_frag = [&](int t, int b) {
-            return *reinterpret_cast<const bf16x8*>(&Vs[(t >> 1) * BLK + ((2 * (t & 1) + lh) * D + b * 32 + lq) * 8]);
+            return *reinterpret_cast<const T8*>(&Vs[(t >> 1) * BLK + ((2 * (t & 1) + lh) * D + b * 32 + lq) * 8]);
         };
-        bf16x8 ka[KS], vfr[2][DB];
+        T8 ka[KS], vfr[2][DB];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) ka[ks] = k_frag(0, ks);
-        if (!ROTATE) rows.init();
+        if (!SCALED) rows.init();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qf[ks], ks ? sacc[kb] : rows.start, 0, 0, 0);
+                sacc[kb] = product(ka[ks], qf[ks][0], ks ? sacc[kb] : rows.start);
+                if (QP == 2) sacc[kb] = product(ka[ks], qf[ks][QP - 1], sacc[kb]);
                 if (kb == 0) ka[ks] = k_frag(1, ks);
                 else if (ks < 2 * DB) vfr[ks / DB][ks % DB] = v_frag(ks / DB, ks % DB);
                 const int step = kb * KS + ks;
@@ -734,13 +810,13 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
                     sacc[kb][x] = (uint32_t)(pos - from) < reach ? sacc[kb][x] : -INFINITY;
                 }
         }
-        bf16x8 pf[4];
-        rows.weigh(sacc, a.scale_log2, o, pf);
+        T8 pf[4];
+        rows.weigh(sacc, row_scale, o, pf);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int b = 0; b < DB; ++b) {
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfr[t & 1][b], pf[t], o[b], 0, 0, 0);
+                o[b] = product(vfr[t & 1][b], pf[t], o[b]);
                 if (t + 2 < 4) vfr[t & 1][b] = v_frag(t + 2, b);
             }
         }

@@ -172,7 +172,10 @@ int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const vo
                           void* workspace, size_t workspace_bytes, void* stream) try {
     if (!batch || !cache_ok(kv) || !rope_ok(rope, rope_positions)) return BZ_EINVAL;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads || n_q_heads > 1024 || window < 0) return BZ_EINVAL;
-    if (!(scale >= 0.f) || !std::isfinite(scale)) return BZ_EINVAL;
+    if (!(scale >= 0.f)) return BZ_EINVAL;
+    // of scores in base 2; a product that vanished would make a NaN of a masked score
+    const float scale_log2 = (scale > 0.f ? scale : 1.f / sqrtf((float)kv->head_dim)) * 1.4426950408889634f * kv->k_scale;
+    if (!std::isnormal(scale_log2)) return BZ_EINVAL;
     const int64_t width = (int64_t)n_q_heads * kv->head_dim;
     if (!rows_ok(q, q_stride, width) || !rows_ok(out, out_stride, width)) return BZ_EINVAL;
     if (workspace && !aligned16(workspace)) return BZ_EINVAL;
@@ -193,7 +196,7 @@ int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const vo
     a.rope = PagedRope{rope, rope_positions};
     a.Hq = n_q_heads;
     a.window = window;
-    a.scale_log2 = (scale > 0.f ? scale : 1.f / sqrtf((float)kv->head_dim)) * 1.4426950408889634f * kv->k_scale;
+    a.scale_log2 = scale_log2;
     launch_paged_attention(a, work, kv->dtype == BZ_KV_E4M3, bv, view_of(kv), (float*)workspace, st);
     return launched(batch, st);
 } catch (...) {

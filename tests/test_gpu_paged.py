@@ -1,7 +1,5 @@
 """The paged KV cache through the C ABI: append with rotation, attention over the pages and reading back, against the float64
 oracle, in both builds.  Unless a test says otherwise, cache memory that no position owns holds NaN."""
-import itertools
-
 import numpy as np
 import pytest
 
@@ -327,6 +325,31 @@ def test_attention_of_large_scores(torch, e4m3):
         want, moved = P.attention(w.qkv64[a:b, :w.Hq * w.d].reshape(n, w.Hq, w.d), k, v, before + np.arange(n), there, 0.125)
         tol = HALF_BF16 * np.abs(want) + moved(2 * (64 + 515) * HALF_F32, HALF_BF16 + 2 * 579 * HALF_F32) * (1 + 2 ** -4)
         assert np.max(np.abs(got[a:b] - want) / tol) <= 1
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rope", [True, False], ids=["rope", "plain"])
+@pytest.mark.parametrize("power", [0, 45, -60, 100])
+def test_e4m3_attention_of_any_query_size(torch, d, rope, power):
+    """Queries far from one, keys as far the other way, so that scores are ordinary; every third token's queries 2^-30 of the
+    others' and every third's with one pair 2^12 above the rest; a token of zeros."""
+    w = World(torch, [(1, 300), (90, 700), (3, 515), (300, 40)], 8, 2, d, 64, e4m3=True, rope=rope, seed=7, scales=(0.02, 0.03))
+    f = 2.0 ** power
+    q, k = w.qkv64[:, :8 * d], w.qkv64[:, 8 * d:10 * d]
+    q *= f
+    q[1::3] *= 2.0 ** -30
+    big = q.reshape(w.T, 8, d)[2::3]                         # a view
+    big *= 2.0 ** -12
+    big[..., 5] *= 2.0 ** 12
+    q[7] = 0
+    k /= f
+    w.qkv = U.to_device(U.W.bf16_bits_from_f32(w.qkv64.astype(np.float32)), False)
+    assert np.array_equal(U.f64(U.W.bf16_bits_from_f32(w.qkv64.astype(np.float32))), w.qkv64)
+    w.q, w.k, w.v = (w.qkv[:, a * d:b * d] for a, b in ((0, 8), (8, 10), (10, 12)))
+    w.scales = (float(np.float32(0.02)) / f, 0.03)
+    w.kv = w.lib.PagedKv(64, 2, d, k=w.dk, v=w.dv, page_table=w.dtable, k_scale=w.scales[0], v_scale=0.03)
+    w.write_new()
+    w.check(w.attend())
 
 
 def w_rounded(torch, x):

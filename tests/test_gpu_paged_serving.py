@@ -350,3 +350,16 @@ def test_a_layer_by_single_operations_agrees_with_run_layers(torch):
             assert U.rel_err(U.from_device(got), want) <= U.BF16_TOL
             U.assert_rms(U.from_device(got), want, U.RMS_BF16)
     inst.close()
+
+
+def test_scales_that_vanish_or_overflow_are_refused(torch):
+    """scale times k_scale has to be a normal float: at 0 a masked score, minus infinity, would become a NaN."""
+    w = World(torch, [(1, 63), (50, 30)], 4, 2, 64, 32, e4m3=True, seed=71, scales=(2.0 ** -100, 0.03))
+    w.write_new()
+    assert torch.isfinite(w.attend(scale=2.0 ** -20).float()).all()
+    for scale in (2.0 ** -30, 1e-45):
+        with pytest.raises(w.lib.BzError):
+            w.attend(scale=scale)
+    w.kv = w.lib.PagedKv(32, 2, 64, k=w.dk, v=w.dv, page_table=w.dtable, k_scale=2.0 ** 100, v_scale=0.03)
+    with pytest.raises(w.lib.BzError):
+        w.attend(scale=2.0 ** 28)
