@@ -90,8 +90,10 @@ __device__ __forceinline__ void rotate(float (&lo)[VEC], float (&hi)[VEC], const
 
 // ---------------------------------------------------------------------------------------------
 // Append.  Sequences with several new tokens: one workgroup per block of 32 positions and `heads_per_wg` heads.  Single new tokens:
-// workgroups from `block_wgs` on, `row_wgs` per token, a thread per 8 rotation pairs or 8 values.  Bound by bytes, single tokens by
-// the launch.
+// workgroups from `block_wgs` on, `row_wgs` per token, a thread per 8 rotation pairs or 8 values.  Bound by bytes, each moved once
+// (12000 tokens on 40 kv heads, bf16: 97 us, 4.0 TB/s, where a large copy has 4.7); a single token by the launch (2.4 us), many by the
+// lines that they touch: a value is one element of each of d pieces of 16 bytes (161 tokens on 32 heads, e4m3: 8.8 us for 10.5 MB of lines
+// in which 0.66 MB change).
 // ---------------------------------------------------------------------------------------------
 constexpr int kAppendBlocks = kPrefillTileQ / 32 + 1;        // blocks that 128 tokens may touch
 
@@ -239,7 +241,8 @@ void launch_paged_append(const act_t* k, size_t k_stride, const act_t* v, size_t
 }
 
 // ---------------------------------------------------------------------------------------------
-// Read: one workgroup per block of 32 positions and `heads_per_wg` heads.  Bound by bytes.
+// Read: one workgroup per block of 32 positions and `heads_per_wg` heads.  Bound by bytes (16000
+// positions on 40 heads, e4m3 to bf16: 103 us, 4.8 TB/s, what a large copy has).
 // ---------------------------------------------------------------------------------------------
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedView kv, int row, int pos0, int n, bf16* __restrict__ k, bf16* __restrict__ v,

@@ -105,8 +105,9 @@ __device__ __forceinline__ float pair_sum(float x) {
 }
 
 // The softmax of a tile of 64 keys for rows that lane pairs own, against a reference that only has to be within 2^kLag of the
-// largest score so far: then most tiles leave the accumulators alone.  Weights are at most 2^kLag, and the row's largest at
-// least 1 when the reference was set; everything is relative to it and no bits are lost.
+// largest score so far: then most tiles leave the accumulators alone.  The row's largest weight is 2^TOP when the reference is set,
+// and weights are at most 2^(TOP + kLag): everything is relative to it and no bits are lost.  With TOP = 6 fp16, which ends at 2^-24,
+// holds weights down to 2^-30 of the largest.
 constexpr float kLag = 8.f;
 template <int DB, bool SCALED, typename P2, typename P8, int TOP>
 struct RowSoftmax {
@@ -183,7 +184,8 @@ __device__ __forceinline__ float2* partial_sums(float* partial, const PagedWork&
 // Narrow: a workgroup reads one chunk of 256 positions of one kv head once, for up to RT rows.  Each of its four waves takes 64
 // positions, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose
 // row operand is the cache as it lies in memory; rows of the problem are the 32 columns.  The four waves' results are merged through
-// LDS in wave order.  Bound by the cache's bytes.
+// LDS in wave order.  Bound by the cache's bytes (64 sequences of up to 4096 positions on 8 kv heads with four query heads each, bf16:
+// 95.5 us, 5.8 TB/s; a streaming read has 7.1 at best), in few workgroups by one's 6.5 us from launch to end.
 //
 // Queries are kept as the sum of two bf16, rounded after the rotation to 16 bits and not to 8: what the matrix pipe does beside the
 // stream costs little.  With up to eight rows the second parts are columns 8..15, which the first parts leave free, and the scores'
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_narrow_join_kernel(PagedQu
 // 32 (four prompts of 2048 tokens on 8 kv heads with eight query heads each: 305 us, with two 381).
 //
 // Bound by the matrix pipe: those 48 products of random numbers take 1.2 us at the clock that the chip's power allows (25 ns each and
-// SIMD, registers only), a tile 1.3.  The softmax between them is the other wave's time on the SIMD: 32 exponentials, 16 of each of
+// SIMD, registers only), a tile 1.4 per CU.  The softmax between them is the other wave's time on the SIMD: 32 exponentials, 16 of each of
 // maximum, conversion and sum.  Its pieces that pay: a reference that lags the maximum (above), taken off by the product
 // itself, which starts from it; the tile's sum as a product with ones.
 // ---------------------------------------------------------------------------------------------
