@@ -844,6 +844,10 @@ int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
     for (bz_batch::Use& u : b->runs) {
         if (u.st == st) continue;
         if (u.unmarked) {
+            bool capturing = false;
+            const int rc = stream_is_capturing(u.st, &capturing);
+            if (rc) return rc;
+            if (capturing) return BZ_ESTATE;             // the event would be the graph's, and `st` would join the capture
             HIP_TRY(hipEventRecord(u.ev, u.st));
             u.unmarked = false;
         }

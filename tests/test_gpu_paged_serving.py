@@ -363,3 +363,43 @@ def test_scales_that_vanish_or_overflow_are_refused(torch):
     w.kv = w.lib.PagedKv(32, 2, 64, k=w.dk, v=w.dv, page_table=w.dtable, k_scale=2.0 ** 100, v_scale=0.03)
     with pytest.raises(w.lib.BzError):
         w.attend(scale=2.0 ** 28)
+
+
+def test_rebuild_while_a_stream_that_ran_the_batch_is_captured(torch):
+    """The rebuild has to follow the attention on the other stream, which cannot be asked for its end under capture: refused, and
+    the capture goes on; afterwards it succeeds."""
+    import paper_2412_17246_amd as lib
+    L = lib.load_library()
+    w = World(torch, [(1, 100)], 4, 2, 64, 32, seed=72)
+    w.write_new()
+    bytes_ = int(L.bz_batch_storage_bytes(1, 1, 256))
+    storage = (torch.empty(bytes_, dtype=torch.uint8, device="cuda"), torch.empty(2 * bytes_, dtype=torch.uint8, pin_memory=True),
+               torch.cuda.Stream())
+    w.batch = batch = lib.Batch(L, [0, 1], [0], [100], storage=storage)
+    torch.cuda.synchronize()
+    graph, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    space = w.workspace()
+
+    def attend():
+        out = torch.zeros(1, w.Hq * w.d, dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        w.attend(out=out, workspace=space, stream=st)
+        return out
+
+    want = attend()
+    torch.cuda.synchronize()
+    x = torch.zeros(8, device="cuda")
+    with torch.cuda.graph(graph, stream=st, capture_error_mode="relaxed"):
+        x += 1
+        with pytest.raises(lib.BzError) as e:
+            batch.rebuild([0, 1], [0], [64])
+        assert e.value.name == "BZ_ESTATE"
+    graph.replay()
+    again = attend()
+    torch.cuda.synchronize()
+    assert torch.all(x == 1) and torch.equal(again, want)
+    batch.rebuild([0, 1], [0], [100])
+    again = attend()
+    torch.cuda.synchronize()
+    assert torch.equal(again, want) and torch.any(want != 0)
+    batch.close()
