@@ -474,8 +474,8 @@ typedef struct bz_paged_kv {
     int32_t        n_pages;         /* n_pages * n_kv_heads * page_size / 32 < 2^31 */
     int32_t        page_size;       /* a power of two from 32 to 1024 */
     int32_t        n_rows;
-    int32_t        pages_per_row;   /* pages_per_row * page_size < 2^31 */
-    int32_t        n_kv_heads;
+    int32_t        pages_per_row;   /* pages_per_row * page_size <= 2^30 */
+    int32_t        n_kv_heads;      /* 1 to 1024, query heads too: a multiple of these */
     int32_t        head_dim;        /* 64 or 128 */
     int32_t        dtype;           /* BZ_KV_ACT: activation elements; BZ_KV_E4M3: bytes */
     float          k_scale;         /* BZ_KV_E4M3: positive and finite; BZ_KV_ACT: 1 */

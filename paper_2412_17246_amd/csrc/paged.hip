@@ -17,7 +17,7 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool shape_ok(const bz_paged_kv* kv) {
     if (!kv || kv->n_pages < 1 || kv->n_rows < 1 || kv->pages_per_row < 1 || kv->n_kv_heads < 1 || kv->n_kv_heads > 1024) return false;
     if (kv->page_size < 32 || kv->page_size > 1024 || (kv->page_size & (kv->page_size - 1))) return false;
-    if ((int64_t)kv->pages_per_row * kv->page_size > 0x7fffffffLL) return false;
+    if ((int64_t)kv->pages_per_row * kv->page_size > 1 << 30) return false;     // positions, and a few thousand more, are 32-bit numbers
     if ((int64_t)kv->n_pages * kv->n_kv_heads * (kv->page_size / 32) > 0x7fffffffLL) return false;    // blocks have 32-bit numbers
     if (kv->head_dim != 64 && kv->head_dim != 128) return false;
     if (kv->dtype == BZ_KV_E4M3) return kv->k_scale > 0.f && kv->v_scale > 0.f && std::isfinite(kv->k_scale) && std::isfinite(kv->v_scale) &&

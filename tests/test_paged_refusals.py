@@ -75,3 +75,11 @@ def test_rope_table(positions, d, base):
 def test_rope_table_refusals(positions, d, base):
     with pytest.raises(B.BzError):
         B.rope_table(positions, d, base)
+
+
+def test_rows_of_more_positions_than_kernels_count_are_refused(lib):
+    """A tile that ends behind the last position still has to have a 32-bit number."""
+    assert lib.bz_paged_kv_bytes(C.byref(cache(page_size=64, pages_per_row=1 << 24))) > 0
+    for bad in (dict(page_size=64, pages_per_row=(1 << 24) + 1), dict(page_size=32, pages_per_row=(1 << 26) - 1),
+                dict(page_size=1024, pages_per_row=(1 << 21) - 1)):
+        assert lib.bz_paged_kv_bytes(C.byref(cache(**bad))) == 0
