@@ -10,6 +10,7 @@
 // (behind the sequence, before the window, on a page that is not there) are cleared before the product.
 #include "paged.h"
 
+#include <algorithm>
 #include <cfloat>
 
 namespace bz {
@@ -477,61 +478,6 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
     }
 }
 
-// Joins the chunks of the narrow sequences that have several, in increasing order: D / 4 threads per (token, query head), eight
-// chunks' loads in flight at once.  Bound by the launch and two trips to memory.
-constexpr int kJoinThreads = 128;
-template <int D>
-__global__ __launch_bounds__(kJoinThreads) void paged_narrow_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
-                                                                         float* __restrict__ partial) {
-    constexpr int NB = 8, TPR = D / 4;
-    int i = blockIdx.x, token = 0;
-    if (i >= bv.n_decode) {
-        const int x = i - bv.n_decode;
-        i = bv.n_decode + x / w.short_tokens;
-        token = x % w.short_tokens;
-    }
-    const int h = blockIdx.y * (kJoinThreads / TPR) + threadIdx.x / TPR, j = (threadIdx.x % TPR) * 4;
-    const int s = bv.decode_seqs[i];
-    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
-    if (token >= n || h >= a.Hq) return;
-    int nch = (before + n - (first_seen(before, a.window) & ~63) + kDecodeChunk - 1) / kDecodeChunk;
-    if (nch == 1) return;                                    // the output is there
-    if (nch > w.max_chunks) nch = w.max_chunks;
-    const size_t at = partial_at(w, bv.n_decode, i, token, a.Hq, h, 0);
-    const float* o = partial + at * D + j;
-    const float2* ml = partial_sums(partial, w, bv.n_decode, a.Hq, D) + at;
-    float M = -INFINITY, den = 0.f;
-    f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = 0; c0 < nch; c0 += NB) {
-        float2 mv[NB];
-        f32x4 ov[NB];
-#pragma unroll
-        for (int u = 0; u < NB; ++u) {
-            const int c = c0 + u < nch ? c0 + u : nch - 1;
-            mv[u] = ml[c];
-            ov[u] = *reinterpret_cast<const f32x4*>(o + (size_t)c * D);
-        }
-        float Mb = M;
-#pragma unroll
-        for (int u = 0; u < NB; ++u) Mb = fmaxf(Mb, mv[u].x);
-        const float ref = finite_or_0(Mb), keep = exp2_flush(M - ref);
-        num *= keep;
-        den *= keep;
-        M = Mb;
-        // no branches: behind one every load would be waited for by itself.  A chunk past the end gets weight zero.
-#pragma unroll
-        for (int u = 0; u < NB; ++u) {
-            const float f = c0 + u < nch ? exp2_flush(mv[u].x - ref) : 0.f;
-#pragma unroll
-            for (int z = 0; z < 4; ++z) num[z] = fmaf(ov[u][z], f, num[z]);
-            den = fmaf(mv[u].y, f, den);
-        }
-    }
-    const float inv = den > 0.f ? kv.v_scale / den : 0.f;
-    const bf16x4 y = {(bf16)(num[0] * inv), (bf16)(num[1] * inv), (bf16)(num[2] * inv), (bf16)(num[3] * inv)};
-    *reinterpret_cast<bf16x4*>(a.out + (size_t)(q0 + token) * a.out_stride + h * D + j) = y;
-}
-
 // ---------------------------------------------------------------------------------------------
 // Wide: 128 rows per workgroup, 32 per wave, keys in tiles of 64 through LDS.  S^T = K Q^T, so that a lane pair (lane, lane + 32)
 // owns a row: its maximum and sum need one exchange, the rescale of O^T is a per-lane factor, and P^T goes from the score
@@ -858,13 +804,72 @@ __global__ __launch_bounds__(256, 2) void paged_wide_kernel(PagedQuery a, PagedW
     }
 }
 
-// Joins the key ranges of wide rows, in increasing order: one workgroup per 32 rows of a kv head.
+// ---------------------------------------------------------------------------------------------
+// Joins the pieces: one launch for the chunks of narrow sequences and the key ranges of wide rows, where a batch has both (512 new tokens
+// on 3001 beside 40 single ones: 113.8 us, with a launch each 118).  Bound by the launch and two trips to memory, with many wide rows by the
+// bytes of their partial results.
+// ---------------------------------------------------------------------------------------------
+// Chunks of the narrow sequences that have several, in increasing order: D / 4 threads per (token, query head), eight chunks' loads in
+// flight at once.
+template <int D, int THREADS>
+__device__ __forceinline__ void join_narrow(const PagedQuery& a, const PagedWork& w, const BatchView& bv, const PagedView& kv,
+                                            float* partial, int i) {
+    constexpr int NB = 8, TPR = D / 4;
+    int token = 0;
+    if (i >= bv.n_decode) {
+        const int x = i - bv.n_decode;
+        i = bv.n_decode + x / w.short_tokens;
+        token = x % w.short_tokens;
+    }
+    const int h = blockIdx.y * (THREADS / TPR) + threadIdx.x / TPR, j = (threadIdx.x % TPR) * 4;
+    const int s = bv.decode_seqs[i];
+    const int q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0, before = bv.kv_before[s];
+    if (token >= n || h >= a.Hq) return;
+    int nch = (before + n - (first_seen(before, a.window) & ~63) + kDecodeChunk - 1) / kDecodeChunk;
+    if (nch == 1) return;                                    // the output is there
+    if (nch > w.max_chunks) nch = w.max_chunks;
+    const size_t at = partial_at(w, bv.n_decode, i, token, a.Hq, h, 0);
+    const float* o = partial + at * D + j;
+    const float2* ml = partial_sums(partial, w, bv.n_decode, a.Hq, D) + at;
+    float M = -INFINITY, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = 0; c0 < nch; c0 += NB) {
+        float2 mv[NB];
+        f32x4 ov[NB];
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const int c = c0 + u < nch ? c0 + u : nch - 1;
+            mv[u] = ml[c];
+            ov[u] = *reinterpret_cast<const f32x4*>(o + (size_t)c * D);
+        }
+        float Mb = M;
+#pragma unroll
+        for (int u = 0; u < NB; ++u) Mb = fmaxf(Mb, mv[u].x);
+        const float ref = finite_or_0(Mb), keep = exp2_flush(M - ref);
+        num *= keep;
+        den *= keep;
+        M = Mb;
+        // no branches: behind one every load would be waited for by itself.  A chunk past the end gets weight zero.
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const float f = c0 + u < nch ? exp2_flush(mv[u].x - ref) : 0.f;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) num[z] = fmaf(ov[u][z], f, num[z]);
+            den = fmaf(mv[u].y, f, den);
+        }
+    }
+    const float inv = den > 0.f ? kv.v_scale / den : 0.f;
+    const bf16x4 y = {(bf16)(num[0] * inv), (bf16)(num[1] * inv), (bf16)(num[2] * inv), (bf16)(num[3] * inv)};
+    *reinterpret_cast<bf16x4*>(a.out + (size_t)(q0 + token) * a.out_stride + h * D + j) = y;
+}
+
+// Key ranges of wide rows, in increasing order: 32 rows of a kv head.
 template <int D>
-__global__ __launch_bounds__(256) void paged_wide_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
-                                                              float* __restrict__ partial) {
+__device__ __forceinline__ void join_wide(const PagedQuery& a, const PagedWork& w, const BatchView& bv, const PagedView& kv,
+                                          float* partial, int rows32) {
     const int Hkv = kv.Hkv, G = w.by_group.d, kvh = blockIdx.y;
-    const int64_t total = (int64_t)bv.T * G, at = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-    if (at >= total) return;
+    const int64_t total = (int64_t)bv.T * G, at = (int64_t)rows32 * 32 + (threadIdx.x & 31);
+    if (at >= total || kvh >= Hkv) return;
     const int t = w.by_group.divide((int)at), s = bv.token_seq[t], q0 = bv.q_start[s], n = bv.q_start[s + 1] - q0;
     const int R = n * G, r = (int)at - q0 * G;
     if (n < 2 || R <= w.narrow_limit) return;
@@ -898,6 +903,14 @@ __global__ __launch_bounds__(256) void paged_wide_join_kernel(PagedQuery a, Page
     }
 }
 
+template <int D, bool CHUNKS, bool RANGES>
+__global__ __launch_bounds__(RANGES ? 256 : 128) void paged_join_kernel(PagedQuery a, PagedWork w, BatchView bv, PagedView kv,
+                                                                        float* __restrict__ narrow, float* __restrict__ wide,
+                                                                        int tokens) {
+    if (CHUNKS && (!RANGES || (int)blockIdx.x < tokens)) join_narrow<D, RANGES ? 256 : 128>(a, w, bv, kv, narrow, blockIdx.x);
+    else if (RANGES) join_wide<D>(a, w, bv, kv, wide, blockIdx.x - tokens);
+}
+
 // ---------------------------------------------------------------------------------------------
 static size_t narrow_bytes(const PagedWork& w, const BatchView& bv, int Hq, int d) {
     if (w.max_chunks <= 1) return 0;
@@ -917,7 +930,6 @@ static void launch_wide(const PagedQuery& q, const PagedWork& w, const BatchView
     (void)limit.raise(reinterpret_cast<const void*>(paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), kLds);
     hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), dim3((unsigned)(bv.n_prefill_items * q.Hq * w.splits)), dim3(256), kLds, st, q,
                        w, bv, kv, ws);
-    if (SPLIT) hipLaunchKernelGGL(paged_wide_join_kernel<D>, dim3((unsigned)(((int64_t)bv.T * w.by_group.d + 31) / 32), kv.Hkv), dim3(256), 0, st, q, w, bv, kv, ws);
 }
 
 template <int D, bool E4M3>
@@ -930,18 +942,21 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
         const unsigned grid = (unsigned)((w.list + (n_narrow - w.first) * w.chunks) * kv.Hkv * w.col_tiles);
         auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, FEW> : paged_narrow_kernel<D, E4M3, kNarrowRows, 3>;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
-        if (w.max_chunks > 1) {
-            const unsigned tokens = (unsigned)(bv.n_decode + w.n_short * w.short_tokens);
-            constexpr int HEADS = kJoinThreads / (D / 4);    // of one workgroup
-            hipLaunchKernelGGL(paged_narrow_join_kernel<D>, dim3(tokens, (q.Hq + HEADS - 1) / HEADS), dim3(kJoinThreads), 0, st, q, w, bv, kv, ws);
-        }
     }
+    float* wide = ws ? ws + narrow_bytes(w, bv, q.Hq, D) / sizeof(float) : nullptr;
     if (w.wide_units > 0) {
-        float* wide = ws ? ws + narrow_bytes(w, bv, q.Hq, D) / sizeof(float) : nullptr;
         auto rows = q.rope.tab ? (w.splits > 1 ? launch_wide<D, E4M3, true, true> : launch_wide<D, E4M3, true, false>)
                                : (w.splits > 1 ? launch_wide<D, E4M3, false, true> : launch_wide<D, E4M3, false, false>);
         rows(q, w, bv, kv, wide, st);
     }
+    const bool chunks = n_narrow > 0 && w.max_chunks > 1, ranges = w.wide_units > 0 && w.splits > 1;
+    if (!chunks && !ranges) return;
+    const int threads = ranges ? 256 : 128, heads = threads / (D / 4);       // of one workgroup
+    const int tokens = chunks ? bv.n_decode + w.n_short * w.short_tokens : 0;
+    const int rows32 = ranges ? (int)(((int64_t)bv.T * w.by_group.d + 31) / 32) : 0;
+    const unsigned across = std::max(chunks ? (q.Hq + heads - 1) / heads : 0, ranges ? kv.Hkv : 0);
+    auto join = chunks ? (ranges ? paged_join_kernel<D, true, true> : paged_join_kernel<D, true, false>) : paged_join_kernel<D, false, true>;
+    hipLaunchKernelGGL(join, dim3(tokens + rows32, across), dim3(threads), 0, st, q, w, bv, kv, ws, wide, tokens);
 }
 
 void launch_paged_attention(const PagedQuery& q, const PagedWork& w, bool e4m3, const BatchView& bv, const PagedView& kv, float* ws,
