@@ -502,7 +502,7 @@ struct WideUnit {
 // XCD-aware: workgroups go to the eight XCDs in turn; with a multiple of eight kv heads each XCD takes whole kv heads and walks
 // one after the other, longest key ranges first, so that what runs on it at a time shares the K and V in its L2.  A grid that fits the
 // chip in one go, two workgroups per CU, lasts as long as its busiest CU, which holds an XCD's workgroups c and 32 + c: the second half
-// is walked backwards, long with short (one prompt of 2048 tokens on 32 kv heads: 61 -> 49 us).
+// is walked backwards, long with short (one prompt of 2048 tokens on 32 kv heads: 77 -> 61 us).
 __device__ __forceinline__ WideUnit wide_unit(int b, int n_items, int subs, int Hkv, int splits) {
     const int per_head = n_items * subs * splits;
     WideUnit u;

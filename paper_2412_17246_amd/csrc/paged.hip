@@ -97,10 +97,10 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
         units += (rows + kWideRows - 1) / kWideRows * Hkv;
         keys = std::max(keys, keys_of((int64_t)b->kv_before[s] + n - std::min<int64_t>(n, kWideRows / G + 1), std::min<int64_t>(n, kWideRows / G + 1), window));
     }
-    // Ranges of the keys: one workgroup per CU, or two where a range keeps twelve tiles of 64 keys.  Two on a CU run a quarter faster
-    // than one, but every range costs its rows' partial results twice; and one range, which needs none, has a launch less, too.
-    // (us with 256 / 512 workgroups: 128 rows on 8000 keys 33 / 40, 512 on 3001 46 / 45, 16 drafts of 10 to 16 tokens 70 / 57,
-    // 1000 rows on 2000 keys, 250 workgroups in one range, 54 / 57.)
+    // Ranges of the keys: one workgroup per CU, or two where a range keeps twelve tiles of 64 keys.  Two on a CU hide each other's waits,
+    // but every range costs its rows' partial results twice; and one range, which needs none, has a launch less, too.
+    // (us with 256 / 512 workgroups: 128 rows on 8000 keys 38 / 44, 512 on 3001 53 / 53, 16 drafts of 10 to 16 tokens 79 / 57,
+    // 1000 rows on 2000 keys, 250 workgroups in one range, 67 / 70.)
     const int64_t tiles = (keys + 63) / 64;
     const auto ranges = [&](int64_t n) { return units ? std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(n / units, 16), tiles / 4)) : 1; };
     w.splits = (int)ranges(256);
