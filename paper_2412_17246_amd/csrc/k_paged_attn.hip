@@ -191,7 +191,7 @@ __device__ __forceinline__ float2* partial_sums(float* partial, const PagedWork&
 // Queries are kept as the sum of two bf16, rounded after the rotation to 16 bits and not to 8: what the matrix pipe does beside the
 // stream costs little.  With up to eight rows the second parts are columns 8..15, which the first parts leave free, and the scores'
 // two parts are added across lanes; with more they are products of their own.  The output's distance from a computation in 64 bits is
-// 2.2e-3 that way (rms, bf16's own rounding of the output 1.7e-3), against 2.7e-3 with queries of one bf16; the rest is the weights,
+// 2.1e-3 that way (rms, bf16's own rounding of the output 1.7e-3), against 2.7e-3 with queries of one bf16; the rest is the weights,
 // which are rounded to bf16 for the product.
 //
 // A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d cache elements: a sixteenth of the bytes

@@ -178,6 +178,7 @@ int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const vo
     if (!std::isnormal(scale_log2)) return BZ_EINVAL;
     const int64_t width = (int64_t)n_q_heads * kv->head_dim;
     if (!rows_ok(q, q_stride, width) || !rows_ok(out, out_stride, width)) return BZ_EINVAL;
+    if (q == out && q_stride != out_stride && batch->T > 1) return BZ_EINVAL;      // a row would overwrite another's query
     if (workspace && !aligned16(workspace)) return BZ_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     int rc = lengths_ok(batch, kv, rope, rope_positions);

@@ -403,3 +403,20 @@ def test_rebuild_while_a_stream_that_ran_the_batch_is_captured(torch):
     torch.cuda.synchronize()
     assert torch.equal(again, want) and torch.any(want != 0)
     batch.close()
+
+
+def test_output_over_the_queries_with_another_pitch_is_refused(torch):
+    """In place means row by row: with another pitch the first rows would overwrite queries that are still to be read."""
+    w = World(torch, [(1, 63), (50, 30)], 4, 2, 64, 32, seed=73)
+    w.write_new()
+    L, ws = w.lib.load_library(), w.workspace()
+    before = w.qkv.clone()
+    call = lambda pitch: L.bz_op_paged_attention(w.batch.handle, w.kv._ref, w.q.data_ptr(), w.row, w.q.data_ptr(), pitch, 4, 0.0, 0,  # noqa: E731
+                                                 w.rope.data_ptr(), w.rope.shape[0], ws.data_ptr(), ws.numel(), None)
+    assert call(w.row - 8) == -1 and call(256) == -1
+    torch.cuda.synchronize()
+    assert torch.equal(w.qkv, before)
+    want = w.attend()
+    assert call(w.row) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(w.q, want)
