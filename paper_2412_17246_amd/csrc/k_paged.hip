@@ -91,9 +91,9 @@ __device__ __forceinline__ void rotate(float (&lo)[VEC], float (&hi)[VEC], const
 // ---------------------------------------------------------------------------------------------
 // Append.  Sequences with several new tokens: one workgroup per block of 32 positions and `heads_per_wg` heads.  Single new tokens:
 // workgroups from `block_wgs` on, `row_wgs` per token, a thread per 8 rotation pairs or 8 values.  Bound by bytes, each moved once
-// (12000 tokens on 40 kv heads, bf16: 97 us, 4.0 TB/s, where a large copy has 4.7); a single token by the launch (2.4 us), many by the
-// lines that they touch: a value is one element of each of d pieces of 16 bytes (161 tokens on 32 heads, e4m3: 8.8 us for 10.5 MB of lines
-// in which 0.66 MB change).
+// (12000 tokens on 40 kv heads, bf16: 97 us, 4.0 TB/s, where a large copy has 4.7); a single token by the launch (2.3 us), many by the
+// lines that they touch: a value is one element of each of d pieces of 16 bytes (161 tokens on 32 heads, e4m3: 6.4 us for 10.5 MB of lines
+// in which 0.66 MB change; with eight neighbouring head dims to a thread, every store 64 lines, 8.9).
 // ---------------------------------------------------------------------------------------------
 constexpr int kAppendBlocks = kPrefillTileQ / 32 + 1;        // blocks that 128 tokens may touch
 
@@ -134,12 +134,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const bf16* __restric
                 *reinterpret_cast<u32x4*>(kc + (at + k_block_offset<false>(p, D / 2 + j)) * 2) = pack<false>(hi, 1.f);
             }
         } else if ((unit -= Hkv * KU) < Hkv * VU) {
-            const int head = unit / VU, j = (unit - head * VU) * 8;
+            // neighbouring threads have neighbouring head dims: a wave's store touches few lines
+            const int head = unit / VU, j = unit - head * VU;
+            const bf16* src = v + (size_t)t * v_stride + head * D + j;
             float x[8];
-            load_row(v + (size_t)t * v_stride + head * D + j, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)src[e * VU];
             const size_t at = block_base(kv, id, head, pos);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cache_put<E4M3>(kv.v, at + v_block_offset<E4M3>(p, j + e, D), E4M3 ? x[e] * kv.v_inv : x[e]);
+            for (int e = 0; e < 8; ++e) cache_put<E4M3>(kv.v, at + v_block_offset<E4M3>(p, j + e * VU, D), E4M3 ? x[e] * kv.v_inv : x[e]);
         }
         return;
     }
