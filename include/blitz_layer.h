@@ -293,6 +293,9 @@ int bz_batch_create_in(const bz_batch_desc* desc, void* device_mem, size_t devic
  * the device).  A refused description (BZ_EINVAL, BZ_ECAPACITY) leaves the batch as it was;
  * BZ_ESTATE for a batch that was made by bz_batch_create. */
 int bz_batch_rebuild(bz_batch* batch, const bz_batch_desc* desc, void* stream);
+/* Waits, on the host, for the uploads and runs that read the batch, and frees it.  Where a stream that ran a paged operation on
+ * it (below) is being captured this cannot be known: BZ_ESTATE, or BZ_EHIP if the stream cannot be asked, and the batch stays as
+ * it was, lent memory in use; call again after the capture. */
 int bz_batch_destroy(bz_batch* batch);
 int bz_batch_tokens(const bz_batch* batch);
 /* For a batch in which every sequence has exactly one new token: enqueue, on `inst`'s compute
@@ -521,8 +524,8 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  *
  * Both operations may be captured into a graph.  It replays the batch as it was: rebuilding, advancing or destroying the batch
  * means capturing again, and is not ordered behind replays by the library.  Under capture a batch that was last rebuilt or
- * advanced on another stream is refused (BZ_ESTATE), and so is rebuilding or advancing a batch while a stream that ran one of these
- * operations before is being captured. */
+ * advanced on another stream is refused (BZ_ESTATE), and so is rebuilding, advancing or destroying a batch while a stream that ran
+ * one of these operations before is being captured. */
 size_t bz_op_paged_attention_workspace_bytes(const bz_batch* batch, const bz_paged_kv* kv, int n_q_heads, int window);
 int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const void* q, int64_t q_stride, void* out,
                           int64_t out_stride, int n_q_heads, float scale, int window, const float* rope, int rope_positions,

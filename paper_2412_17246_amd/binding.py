@@ -248,7 +248,8 @@ class Batch:
 
     def __init__(self, lib: C.CDLL, q_start: Sequence[int], seq_slot: Sequence[int], kv_len_before: Sequence[int],
                  storage=None):
-        self._lib = lib
+        _close_collected()
+        self._lib, self.handle = lib, None
         d, keep = _desc(q_start, seq_slot, kv_len_before)
         h = _P()
         self._storage = storage
@@ -275,15 +276,35 @@ class Batch:
         self.B = int(keep[1].size)
 
     def close(self):
+        """Raises, and leaves the batch as it is, while a stream that ran a paged operation on it is being captured."""
+        _close_collected()
         if self.handle:
-            self._lib.bz_batch_destroy(self.handle)
+            rc = self._lib.bz_batch_destroy(self.handle)
+            if rc:
+                raise BzError(rc, "bz_batch_destroy", self._lib.bz_last_hip_error().decode() if rc == -6 else "")
             self.handle = None
 
     def __del__(self):
         try:
-            self.close()
+            if self.handle and self._lib.bz_batch_destroy(self.handle):
+                _collected.append((self._lib, self.handle, self._storage))
         except Exception:
             pass
+
+
+# Batches that were collected when they could not be destroyed, with the memory that their kernels may still read: the next
+# batch that is made or closed tries again.
+_collected: list = []
+
+
+def _close_collected() -> None:
+    for _ in range(len(_collected)):
+        try:
+            kept = _collected.pop()                          # nobody else's now
+        except IndexError:
+            return
+        if kept[0].bz_batch_destroy(kept[1]):
+            _collected.insert(0, kept)
 
 
 class Instance:

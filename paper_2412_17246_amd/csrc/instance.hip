@@ -839,18 +839,24 @@ void bind_batch(bz_batch* b) {
     b->d_work = reinterpret_cast<int4*>(static_cast<unsigned char*>(b->dev) + b->work_at);
 }
 
+// Records the event that single operations left to whoever needs it.  Under capture it would be the graph's: refused.
+int mark_use(bz_batch::Use& u) {
+    if (!u.unmarked) return BZ_OK;
+    bool capturing = false;
+    const int rc = stream_is_capturing(u.st, &capturing);
+    if (rc) return rc;
+    if (capturing) return BZ_ESTATE;
+    HIP_TRY(hipEventRecord(u.ev, u.st));
+    u.unmarked = false;
+    return BZ_OK;
+}
+
 // Orders stream `st` behind every run of the batch that was enqueued on another stream.
 int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
     for (bz_batch::Use& u : b->runs) {
         if (u.st == st) continue;
-        if (u.unmarked) {
-            bool capturing = false;
-            const int rc = stream_is_capturing(u.st, &capturing);
-            if (rc) return rc;
-            if (capturing) return BZ_ESTATE;             // the event would be the graph's, and `st` would join the capture
-            HIP_TRY(hipEventRecord(u.ev, u.st));
-            u.unmarked = false;
-        }
+        const int rc = mark_use(u);
+        if (rc) return rc;
         HIP_TRY(hipStreamWaitEvent(st, u.ev, 0));
     }
     return BZ_OK;
@@ -943,18 +949,19 @@ extern "C" {
 
 int bz_batch_destroy(bz_batch* b) {
     if (!b) return BZ_EINVAL;
-    // an upload still reading the caller's staging, or a kernel still reading the device arrays, must not outlive them
+    // an upload still reading the caller's staging, or a kernel still reading the device arrays, must not outlive them:
+    // where a stream cannot say when it is done with them, the batch stays
+    for (bz_batch::Use& u : b->runs) {
+        const int rc = mark_use(u);
+        if (rc) return rc;
+    }
+    for (const bz_batch::Use& u : b->runs) HIP_TRY(hipEventSynchronize(u.ev));
     for (int h = 0; h < 2; ++h) {
         if (b->staged_valid[h]) (void)hipEventSynchronize(b->staged_ev[h]);
         if (b->staged_ev[h]) (void)hipEventDestroy(b->staged_ev[h]);
     }
     if (b->changed_valid) (void)hipEventSynchronize(b->changed_ev);
-    for (const bz_batch::Use& u : b->runs) {
-        bool capturing = false;
-        if (u.unmarked && stream_is_capturing(u.st, &capturing) == BZ_OK && !capturing) (void)hipEventRecord(u.ev, u.st);
-        (void)hipEventSynchronize(u.ev);
-        (void)hipEventDestroy(u.ev);
-    }
+    for (const bz_batch::Use& u : b->runs) (void)hipEventDestroy(u.ev);
     if (b->changed_ev) (void)hipEventDestroy(b->changed_ev);
     if (b->own_dev && b->dev) (void)hipFree(b->dev);
     delete b;

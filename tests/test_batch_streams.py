@@ -1,0 +1,135 @@
+"""How a batch is ordered between streams, and what is refused, with a stand-in for the HIP runtime (c_abi/hip_standin.c) that keeps
+the books: no GPU, kernels are counted and not run.  Each test is a process of its own, in which the stand-in is loaded first."""
+import inspect
+import os
+import subprocess
+import sys
+import textwrap
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+PRELUDE = """
+import ctypes as C, sys
+from types import SimpleNamespace
+sys.path.insert(0, %r)
+hip = C.CDLL(%r, mode=C.RTLD_GLOBAL)
+from paper_2412_17246_amd import binding as B
+L = B.load_library(%r)
+A, S, T = 0x1000, 0x2000, 0x3000                             # streams
+stream = lambda h: SimpleNamespace(cuda_stream=h)
+for f, ret, args in (("capture", None, [C.c_void_p, C.c_ulonglong]), ("release", None, [C.c_void_p]), ("dead_uses", C.c_int, []),
+                     ("forbidden", C.c_int, []), ("pending", C.c_long, [C.c_void_p]), ("unordered", C.c_long, [C.c_void_p, C.c_void_p]),
+                     ("work", None, [C.c_void_p]), ("launches", C.c_long, []), ("grid", None, [C.c_void_p])):
+    fn = getattr(hip, "standin_" + f)
+    fn.restype, fn.argtypes = ret, args
+class Lent:
+    def __init__(self, n):
+        self.raw = C.create_string_buffer(n + 64)
+        self.n, self.at = n, (C.addressof(self.raw) + 63) // 64 * 64
+    def data_ptr(self): return self.at
+    def numel(self): return self.n
+def lent(st, q_start=(0, 1), slots=(0,), before=(100,), size=1 << 15):
+    return B.Batch(L, q_start, slots, before, storage=(Lent(size), Lent(2 * size), stream(st)))
+KV = B.bz_paged_kv(4096, 8192, 256, 64, 64, 16, 16, 2, 64, B.BZ_KV_ACT, 1.0, 1.0)
+def append(batch, st, kv=KV):
+    width = kv.n_kv_heads * kv.head_dim
+    return L.bz_op_paged_append(batch.handle, C.byref(kv), 4096, width, 8192, width, None, 0, st)
+def rebuild(batch, st):
+    try:
+        batch.rebuild([0, 1], [0], [64], stream=stream(st))
+    except B.BzError as e:
+        return e.status
+    return 0
+EINVAL, ENOMEM, EHIP, ECAPACITY, ESTATE = -1, -2, -6, -7, -8
+"""
+
+
+@pytest.fixture(scope="module")
+def standin(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("standin") / "libstandin.so")
+    subprocess.run(["gcc", "-std=c11", "-O1", "-shared", "-fPIC", "-Wall", "-Wextra", "-Werror",
+                    os.path.join(ROOT, "tests", "c_abi", "hip_standin.c"), "-o", so], check=True)
+    return so
+
+
+def run(standin, scenario, fp32=False):
+    """The body of `scenario`, a function without arguments, in a process of its own."""
+    body = textwrap.dedent(inspect.getsource(scenario).split("():\n", 1)[1])
+    code = PRELUDE % (ROOT, standin, fp32) + body + '\nprint("scenario done")\n'
+    res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100)
+    assert res.returncode == 0 and "scenario done" in res.stdout, res.stdout + res.stderr
+
+
+BUILDS = pytest.mark.parametrize("fp32", [False, True], ids=["bf16", "fp32dbg"])
+
+
+@BUILDS
+def test_destroy_while_a_stream_that_ran_the_batch_is_captured(standin, fp32):
+    """Kernels that were enqueued before the capture may still read the batch, and the stream cannot be asked for their end: refused,
+    and the batch stays as it was."""
+    def scenario():
+        b = lent(A)
+        assert append(b, S) == 0 and append(b, T) == 0
+        hip.standin_capture(S, 7)
+        assert L.bz_batch_destroy(b.handle) == ESTATE and hip.standin_pending(S) > 0
+        assert L.bz_batch_tokens(b.handle) == 1 and append(b, T) == 0
+        hip.standin_capture(S, 0)
+        assert L.bz_batch_destroy(b.handle) == 0 and hip.standin_pending(S) == 0 and hip.standin_pending(T) == 0
+        b.handle = None
+        assert hip.standin_forbidden() == 0 and hip.standin_dead_uses() == 0
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_destroy_when_a_stream_cannot_be_asked(standin, fp32):
+    def scenario():
+        b = lent(A)
+        assert append(b, S) == 0
+        hip.standin_release(S)                                   # too early
+        assert L.bz_batch_destroy(b.handle) == EHIP and L.bz_batch_tokens(b.handle) == 1
+        b.handle = None
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_refused_close_can_be_repeated(standin, fp32):
+    def scenario():
+        b = lent(A)
+        assert append(b, S) == 0
+        hip.standin_capture(S, 7)
+        try:
+            b.close()
+            raise SystemExit("closed")
+        except B.BzError as e:
+            assert e.status == ESTATE and b.handle
+        hip.standin_capture(S, 0)
+        b.close()
+        assert b.handle is None and hip.standin_pending(S) == 0
+        b.close()
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_batch_collected_during_a_capture_is_destroyed_later(standin, fp32):
+    """With its storage kept until then: the next batch that is made or closed tries again."""
+    def scenario():
+        import gc, weakref
+        b = lent(A)
+        memory = weakref.ref(b._storage[0])
+        assert append(b, S) == 0
+        hip.standin_capture(S, 7)
+        del b
+        gc.collect()
+        other = lent(A)
+        assert hip.standin_pending(S) > 0 and memory() is not None
+        hip.standin_capture(S, 0)
+        other.close()
+        gc.collect()
+        assert hip.standin_pending(S) == 0 and memory() is None
+
+    run(standin, scenario, fp32)
