@@ -867,6 +867,15 @@ int mark_changed(bz_batch* b, hipStream_t st) {
     HIP_TRY(hipEventRecord(b->changed_ev, st));
     b->changed_on = st;
     b->changed_valid = true;
+    // this event is behind the stream's own operations as well, and stands for them: the stream may go now.  Not a graph's event,
+    // which nobody outside the graph can wait for.
+    for (bz_batch::Use& u : b->runs) {
+        if (u.st != st || !u.unmarked) continue;
+        bool capturing = false;
+        const int rc = stream_is_capturing(st, &capturing);
+        if (rc) return rc;
+        u.unmarked = capturing;
+    }
     return BZ_OK;
 }
 

@@ -133,3 +133,55 @@ def test_a_batch_collected_during_a_capture_is_destroyed_later(standin, fp32):
         assert hip.standin_pending(S) == 0 and memory() is None
 
     run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_stream_is_not_asked_again_after_a_change_on_it(standin, fp32):
+    """Operations on S, a rebuild on S, S released: what follows is ordered by the rebuild's event."""
+    def scenario():
+        b = lent(A)
+        for turn in range(2):
+            assert append(b, S) == 0
+        assert rebuild(b, S) == 0
+        hip.standin_release(S)
+        assert rebuild(b, T) == 0 and hip.standin_unordered(T, S) == 0
+        assert append(b, T) == 0 and rebuild(b, A) == 0 and hip.standin_unordered(A, T) == 0
+        b.close()
+        assert hip.standin_dead_uses() == 0 and hip.standin_pending(S) == 0 and hip.standin_pending(T) == 0
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_an_instance_that_advanced_the_batch_may_go(standin, fp32):
+    def scenario():
+        import workloads as W
+        cfg = B.make_config(W.CONFIGS["tiny"], max_seqs=1, max_seq_len=64, max_tokens=1, kv_tokens=64)
+        cfg.compute_stream, cfg.copy_stream = S, A
+        inst = C.c_void_p()
+        assert L.bz_create(C.byref(cfg), C.byref(inst)) == 0
+        b = B.Batch(L, [0, 1], [0], [5])
+        assert append(b, S) == 0 and L.bz_batch_advance(inst, b.handle) == 0 and append(b, T) == 0
+        assert hip.standin_unordered(T, S) == 0
+        assert L.bz_destroy(inst) == 0
+        hip.standin_release(S)
+        b.close()
+        assert hip.standin_dead_uses() == 0 and hip.standin_pending(T) == 0
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_change_on_another_stream_still_asks(standin, fp32):
+    """The event of operations on S is recorded for a change on T, and again after more of them; S's own change in between does not
+    stand for what S did later."""
+    def scenario():
+        b = lent(A)
+        assert append(b, S) == 0 and rebuild(b, T) == 0 and hip.standin_unordered(T, S) == 0
+        assert append(b, S) == 0 and rebuild(b, S) == 0 and append(b, S) == 0
+        assert rebuild(b, T) == 0 and hip.standin_unordered(T, S) == 0
+        assert append(b, S) == 0
+        b.close()
+        assert hip.standin_pending(S) == 0 and hip.standin_dead_uses() == 0 and hip.standin_forbidden() == 0
+
+    run(standin, scenario, fp32)
