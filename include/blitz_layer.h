@@ -524,8 +524,9 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  *
  * Both operations may be captured into a graph.  It replays the batch as it was: rebuilding, advancing or destroying the batch
  * means capturing again, and is not ordered behind replays by the library.  Under capture a batch that was last rebuilt or
- * advanced on another stream is refused (BZ_ESTATE), and so is rebuilding, advancing or destroying a batch while a stream that ran
- * one of these operations before is being captured. */
+ * advanced on another stream, outside the graph, is refused (BZ_ESTATE), and so is rebuilding, advancing or destroying a batch
+ * while a stream that ran one of these operations before is being captured.  Where the advance itself is captured, on one stream,
+ * and runs or operations on others, the library orders them inside the graph as it does outside. */
 size_t bz_op_paged_attention_workspace_bytes(const bz_batch* batch, const bz_paged_kv* kv, int n_q_heads, int window);
 int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const void* q, int64_t q_stride, void* out,
                           int64_t out_stride, int n_q_heads, float scale, int window, const float* rope, int rope_positions,

@@ -61,12 +61,15 @@ struct bz_batch {
     // Ordering between streams.  A batch may be run by two instances with different compute streams (a split
     // pair).  Runs that must be ordered against a later device-side change of the batch (advance, rebuild)
     // leave an event per stream; the change leaves one that later runs on other streams wait for.
-    // (`unmarked`: the event is behind by single operations, and is recorded when a change asks for it)
-    struct Use { hipStream_t st; hipEvent_t ev; bool unmarked; };
+    // (`unmarked`: the event is behind by single operations, and is recorded when a change asks for it.)
+    // What is captured has events of its own, good inside its graph alone: `capture` says which, 0 for none.  (`single`: left by
+    // single operations, whose stream exists until the next change.)
+    struct Use { hipStream_t st; hipEvent_t ev; bool unmarked, single; unsigned long long capture; };
     mutable std::vector<Use> runs;
     hipStream_t changed_on = nullptr;
     hipEvent_t changed_ev = nullptr;
     bool changed_valid = false;
+    unsigned long long changed_capture = 0;
 };
 
 namespace bz {
@@ -74,7 +77,7 @@ BatchView batch_view(const bz_batch* b);
 // around the kernels that read a batch on stream `st`
 int batch_before_run(const bz_batch* b, hipStream_t st);
 int batch_after_run(const bz_batch* b, hipStream_t st, bool mark);
-int stream_is_capturing(hipStream_t st, bool* out);
+int capture_of(hipStream_t st, unsigned long long* id);      // 0: none
 }  // namespace bz
 
 struct bz_instance {

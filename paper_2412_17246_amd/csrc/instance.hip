@@ -839,24 +839,29 @@ void bind_batch(bz_batch* b) {
     b->d_work = reinterpret_cast<int4*>(static_cast<unsigned char*>(b->dev) + b->work_at);
 }
 
-// Records the event that single operations left to whoever needs it.  Under capture it would be the graph's: refused.
+// Records the event that single operations left to whoever needs it.  Under capture it would be the graph's: refused, and so is
+// a change outside the graph while operations on the stream are being captured.
 int mark_use(bz_batch::Use& u) {
-    if (!u.unmarked) return BZ_OK;
-    bool capturing = false;
-    const int rc = stream_is_capturing(u.st, &capturing);
+    if (!(u.capture ? u.single : u.unmarked)) return BZ_OK;
+    unsigned long long now = 0;
+    const int rc = capture_of(u.st, &now);
     if (rc) return rc;
-    if (capturing) return BZ_ESTATE;
-    HIP_TRY(hipEventRecord(u.ev, u.st));
-    u.unmarked = false;
+    if (u.capture ? now == u.capture : now != 0) return BZ_ESTATE;
+    if (!u.capture) HIP_TRY(hipEventRecord(u.ev, u.st));
+    u.unmarked = u.single = false;
     return BZ_OK;
 }
 
 // Orders stream `st` behind every run of the batch that was enqueued on another stream.
 int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
+    unsigned long long capture = 0;
+    int rc = b->runs.empty() ? BZ_OK : capture_of(st, &capture);
+    if (rc) return rc;
     for (bz_batch::Use& u : b->runs) {
         if (u.st == st) continue;
-        const int rc = mark_use(u);
-        if (rc) return rc;
+        const bool same_graph = u.capture && u.capture == capture;
+        if (!same_graph && (rc = mark_use(u)) != BZ_OK) return rc;
+        if (u.capture && !same_graph) continue;              // replays are the caller's to order
         HIP_TRY(hipStreamWaitEvent(st, u.ev, 0));
     }
     return BZ_OK;
@@ -864,18 +869,15 @@ int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
 
 int mark_changed(bz_batch* b, hipStream_t st) {
     if (!b->changed_ev) HIP_TRY(hipEventCreateWithFlags(&b->changed_ev, hipEventDisableTiming));
+    const int rc = capture_of(st, &b->changed_capture);
+    if (rc) return rc;
     HIP_TRY(hipEventRecord(b->changed_ev, st));
     b->changed_on = st;
     b->changed_valid = true;
-    // this event is behind the stream's own operations as well, and stands for them: the stream may go now.  Not a graph's event,
-    // which nobody outside the graph can wait for.
-    for (bz_batch::Use& u : b->runs) {
-        if (u.st != st || !u.unmarked) continue;
-        bool capturing = false;
-        const int rc = stream_is_capturing(st, &capturing);
-        if (rc) return rc;
-        u.unmarked = capturing;
-    }
+    // this event is behind the stream's own operations as well, and stands for them: the stream may go now.  A graph's event stands
+    // for the graph's alone.
+    for (bz_batch::Use& u : b->runs)
+        if (u.st == st && (u.capture != 0) == (b->changed_capture != 0)) u.unmarked = u.single = false;
     return BZ_OK;
 }
 
@@ -912,43 +914,46 @@ BatchView batch_view(const bz_batch* b) {
 // Orders stream `st` behind the batch's last change if that was enqueued on another stream.
 int batch_before_run(const bz_batch* b, hipStream_t st) {
     if (!b->changed_valid || b->changed_on == st) return BZ_OK;
-    bool capturing = false;
-    const int rc = stream_is_capturing(st, &capturing);
+    unsigned long long capture = 0;
+    const int rc = capture_of(st, &capture);
     if (rc) return rc;
-    if (capturing) return BZ_ESTATE;         // the wait would be for work outside the capture
+    if (capture && capture != b->changed_capture) return BZ_ESTATE;      // the wait would be for work outside the graph
     HIP_TRY(hipStreamWaitEvent(st, b->changed_ev, 0));
     return BZ_OK;
 }
 
 // A batch that can change on the device later (advance, rebuild), possibly on another stream, gets a marker behind the
-// kernels that read it: one event per stream that ever ran it.  bz_run_layers records it again after every run; after a single
-// operation, which takes as little as 3 us, recording would cost another 3 us of the host's time and is left to the change.
+// kernels that read it: one event per stream that ever ran it, and one for what was captured there.  bz_run_layers records it again
+// after every run; after a single operation, which takes as little as 3 us, recording would cost another 3 us of the host's time and is
+// left to the change.  Under capture, where the host's time does not count, it is recorded at once: the change may be captured, too.
 int batch_after_run(const bz_batch* b, hipStream_t st, bool mark) {
     if (!b->all_decode && !b->staging) return BZ_OK;
-    bool capturing = false;
-    const int rc = stream_is_capturing(st, &capturing);
+    unsigned long long capture = 0;
+    const int rc = capture_of(st, &capture);
     if (rc) return rc;
-    if (capturing) return BZ_OK;             // replays are the caller's to order
     bz_batch::Use* use = nullptr;
     for (bz_batch::Use& u : b->runs)
-        if (u.st == st) use = &u;
+        if (u.st == st && (u.capture != 0) == (capture != 0)) use = &u;
     if (!use) {
         hipEvent_t ev = nullptr;
         HIP_TRY(hipEventCreateWithFlags(&ev, hipEventDisableTiming));
-        b->runs.push_back(bz_batch::Use{st, ev, false});
+        b->runs.push_back(bz_batch::Use{st, ev, false, false, capture});
         use = &b->runs.back();
     }
-    use->unmarked = !mark;
-    if (mark) HIP_TRY(hipEventRecord(use->ev, st));
+    use->single = !mark || (use->single && use->capture == capture && capture);
+    use->unmarked = !mark && !capture;
+    use->capture = capture;
+    if (mark || capture) HIP_TRY(hipEventRecord(use->ev, st));
     return BZ_OK;
 }
 
-int stream_is_capturing(hipStream_t st, bool* out) {
-    *out = false;
+int capture_of(hipStream_t st, unsigned long long* id) {
+    *id = 0;
     if (!st) return BZ_OK;                   // the null stream cannot be captured
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    HIP_TRY(hipStreamIsCapturing(st, &status));
-    *out = status != hipStreamCaptureStatusNone;
+    unsigned long long at = 0;
+    HIP_TRY(hipStreamGetCaptureInfo(st, &status, &at));
+    if (status != hipStreamCaptureStatusNone) *id = at;
     return BZ_OK;
 }
 
@@ -964,12 +969,13 @@ int bz_batch_destroy(bz_batch* b) {
         const int rc = mark_use(u);
         if (rc) return rc;
     }
-    for (const bz_batch::Use& u : b->runs) HIP_TRY(hipEventSynchronize(u.ev));
+    for (const bz_batch::Use& u : b->runs)
+        if (!u.capture) HIP_TRY(hipEventSynchronize(u.ev));
+    if (b->changed_valid && !b->changed_capture) HIP_TRY(hipEventSynchronize(b->changed_ev));
     for (int h = 0; h < 2; ++h) {
         if (b->staged_valid[h]) (void)hipEventSynchronize(b->staged_ev[h]);
         if (b->staged_ev[h]) (void)hipEventDestroy(b->staged_ev[h]);
     }
-    if (b->changed_valid) (void)hipEventSynchronize(b->changed_ev);
     for (const bz_batch::Use& u : b->runs) (void)hipEventDestroy(u.ev);
     if (b->changed_ev) (void)hipEventDestroy(b->changed_ev);
     if (b->own_dev && b->dev) (void)hipFree(b->dev);

@@ -185,3 +185,82 @@ def test_a_change_on_another_stream_still_asks(standin, fp32):
         assert hip.standin_pending(S) == 0 and hip.standin_dead_uses() == 0 and hip.standin_forbidden() == 0
 
     run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_graph_over_two_streams_orders_a_batch_within_itself(standin, fp32):
+    """Steps of a split pair captured into one graph: each half on its own stream, the batch advanced in between."""
+    def scenario():
+        import workloads as W
+        s = W.CONFIGS["tiny"]
+        pair = []
+        for st in (S, T):
+            cfg = B.make_config(s, max_seqs=1, max_seq_len=64, max_tokens=1, kv_tokens=64)
+            cfg.compute_stream, cfg.copy_stream = st, A
+            inst, sizes = C.c_void_p(), B.bz_sizes()
+            assert L.bz_create(C.byref(cfg), C.byref(inst)) == 0 and L.bz_query_sizes(C.byref(cfg), C.byref(sizes)) == 0
+            blob = C.create_string_buffer(sizes.layer_bytes)
+            for l in range(s.L):
+                assert L.bz_load_layer(inst, l, blob, sizes.layer_bytes) == 0
+            assert L.bz_kv_reserve(inst, 0, 64) == 0 and L.bz_frontier(inst) == s.L
+            pair.append(inst)
+        b, hidden = B.Batch(L, [0, 1], [0], [5]), C.create_string_buffer(4 * s.H)
+        hip.standin_capture(S, 7)
+        for step in range(3):
+            assert L.bz_run_layers(pair[0], 0, 1, b.handle, hidden, 0) == 0
+            assert L.bz_signal_stream(pair[0], T) == 0           # the hidden states
+            hip.standin_work(S)
+            assert L.bz_run_layers(pair[1], 1, 2, b.handle, hidden, 0) == 0
+            assert hip.standin_unordered(S, T) > 0
+            assert L.bz_batch_advance(pair[0], b.handle) == 0
+            assert hip.standin_unordered(S, T) == 0
+        assert hip.standin_forbidden() == 0
+        hip.standin_capture(S, 0); hip.standin_capture(T, 0)
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_graph_of_single_operations_orders_a_batch_within_itself(standin, fp32):
+    """Operations on S, the batch advanced on A, one graph; a second graph knows nothing of the first."""
+    def scenario():
+        import workloads as W
+        cfg = B.make_config(W.CONFIGS["tiny"], max_seqs=1, max_seq_len=64, max_tokens=1, kv_tokens=64)
+        cfg.compute_stream, cfg.copy_stream = A, T
+        inst = C.c_void_p()
+        assert L.bz_create(C.byref(cfg), C.byref(inst)) == 0
+        b = lent(A)
+        hip.standin_capture(A, 7); hip.standin_capture(S, 7)
+        assert append(b, S) == ESTATE                            # the last change was no part of the graph
+        assert L.bz_batch_advance(inst, b.handle) == 0
+        for turn in range(3):
+            assert append(b, S) == 0 and hip.standin_unordered(S, A) == 0 and hip.standin_unordered(A, S) > 0
+            assert L.bz_batch_advance(inst, b.handle) == 0 and hip.standin_unordered(A, S) == 0
+        hip.standin_capture(A, 0); hip.standin_capture(S, 8)
+        assert append(b, S) == ESTATE
+        hip.standin_capture(S, 0)
+        assert hip.standin_forbidden() == 0
+
+    run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_change_outside_a_graph_that_is_being_captured(standin, fp32):
+    """Operations on S were captured and S still is: a change or the end of the batch would have to follow what never ran."""
+    def scenario():
+        b = lent(S)
+        hip.standin_capture(S, 7)
+        assert append(b, S) == 0 and rebuild(b, T) == ESTATE
+        try:
+            b.close()
+            raise SystemExit("closed")
+        except B.BzError as e:
+            assert e.status == ESTATE
+        hip.standin_capture(S, 0)
+        assert rebuild(b, T) == 0                                # replays are the caller's to order
+        hip.standin_release(S)
+        assert append(b, T) == 0 and rebuild(b, A) == 0
+        b.close()
+        assert hip.standin_dead_uses() == 0 and hip.standin_forbidden() == 0
+
+    run(standin, scenario, fp32)
