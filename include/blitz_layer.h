@@ -512,8 +512,9 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  * rotated query, for the product with the keys, to two bf16 whose sum it is.  Over BZ_KV_E4M3, in sequences whose new tokens times
  * n_q_heads / n_kv_heads exceed 32, weights and queries are fp16 instead: 11 bits, and elements of a query below 2^-38 of its
  * largest count as nothing.
- * A value that is not finite shows in every query that sees it, and may show in queries of the same sequence and call that come
- * before it; in no other sequence.
+ * A value that is not finite shows in every query that sees it, and may show in other queries of the same sequence and call:
+ * those before it, and with a window those that have left it behind.  It does in no other sequence, nor in a call none of whose
+ * queries sees it.  A key that is not finite shows in the queries that see it alone.
  * `workspace`: device scratch, 16-byte aligned, of at least bz_op_paged_attention_workspace_bytes() bytes for the same batch,
  * shapes and window (BZ_ENOMEM if smaller); calls that may overlap in time need workspaces of their own.
  * Results depend within rounding on the other sequences of the batch, whose lengths say how key ranges are cut; the same call

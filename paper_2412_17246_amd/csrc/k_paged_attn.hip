@@ -7,7 +7,8 @@
 // has m = -inf, l = 0.
 //
 // Masked positions get weight 0, and 0 times a NaN is a NaN: values at positions that none of the workgroup's rows may see
-// (behind the sequence, before the window, on a page that is not there) are cleared before the product.
+// (behind the sequence, before the first row's window, on a page that is not there) are cleared before the product.  One that some of
+// them see and that is not finite reaches the others as well: to tell them apart would cost every tile that a mask crosses.
 #include "paged.h"
 
 #include <algorithm>

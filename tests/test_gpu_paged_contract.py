@@ -1,8 +1,10 @@
 """What the paged KV cache's operations promise beside their results: when a batch may go, what is refused before a launch, how far a
 value that is not finite reaches, how precise queries and sums are."""
+import numpy as np
 import pytest
 
-from tests.test_gpu_paged import World
+from oracle import paged as P
+from tests.test_gpu_paged import CACHES, World
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +46,38 @@ def test_destroy_while_a_stream_that_ran_the_batch_is_captured(torch):
     assert torch.all(x == 1) and torch.equal(out, want) and torch.any(want != 0)
     batch.close()
     assert batch.handle is None
+
+
+@CACHES
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2)], ids=lambda h: "x".join(map(str, h)))
+@pytest.mark.parametrize("n", [3, 90, 300], ids=["draft", "wide", "tiles"])
+def test_a_value_that_is_not_finite_under_a_window(torch, e4m3, heads, n):
+    """Every query that sees it shows it; other sequences do not, nor do queries once the window of every query of the call has
+    left it; what other queries of its sequence and call show is left open."""
+    window, d = 64, 128
+    seqs = [(1, 200), (n, 100), (1, 90), (2, 130)]
+    w = World(torch, seqs, *heads, d, 32, e4m3=e4m3, seed=87)
+    w.write_new()
+    want = w.attend(window=window)
+    a, b, pos = w.q_start[1], w.q_start[2], 100 + np.arange(n)
+
+    def with_nan_at(at):
+        place = P.places(w.table[1], [at], heads[1], 32, d, w.piece)[1]
+        was, w.hv[place] = w.hv[place], np.nan               # which e4m3 has, too
+        w.dv.copy_(w.upload(w.hv))
+        w.hv[place] = was
+        return w.attend(window=window)
+
+    got = with_nan_at(70)
+    same = torch.eq(got.view(torch.int16), want.view(torch.int16)).all(dim=1)
+    assert torch.all(same[:a]) and torch.all(same[b:])
+    sees = torch.from_numpy((pos >= 70) & (pos - window < 70)).cuda()
+    assert sees.any() and torch.isnan(got[a:b][sees]).all()
+    assert torch.equal(with_nan_at(20), want)                # before the first query's window
+    w.dv.copy_(w.upload(w.hv))
+    place = P.places(w.table[1], [70], heads[1], 32, d, w.piece)[0]
+    w.hk[place] = np.nan
+    w.dk.copy_(w.upload(w.hk))
+    got = w.attend(window=window)                            # a key reaches those that see it alone
+    same = torch.eq(got.view(torch.int16), want.view(torch.int16)).all(dim=1)
+    assert torch.all(same[:a]) and torch.all(same[b:]) and torch.equal(same[a:b], ~sees) and torch.isnan(got[a:b][sees]).all()
