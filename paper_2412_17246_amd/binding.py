@@ -761,6 +761,8 @@ def op_paged_attention(batch: Batch, kv: PagedKv, q, out, scale: float = 0.0, wi
     width = _rows(kv, batch, q, "q")
     if _rows(kv, batch, out, "out") != width or width % kv.head_dim:
         raise ValueError("a row of q and out must be n_q_heads * head_dim elements")
+    if workspace is not None and (workspace.device != kv._device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
     tab, positions = _rope(kv, rope)
     rc = kv.lib.bz_op_paged_attention(batch.handle, kv._ref, q.data_ptr(), _pitch(q), out.data_ptr(), _pitch(out),
                                       width // kv.head_dim, scale, window, tab, positions,

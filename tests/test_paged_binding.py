@@ -1,0 +1,44 @@
+"""What the binding of the paged operations refuses before the library sees it: tensors of the host in place of the GPU's, and a library
+that must not be reached."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2412_17246_amd import binding as B
+
+
+@pytest.fixture
+def call(monkeypatch):
+    """An attention over a cache "on" the host, with arguments replaced; its calls of the library are counted."""
+    monkeypatch.setattr(B, "_on_device", lambda kv: None)
+    reached = []
+
+    def attention(*a):
+        reached.append(a)
+        return 0
+
+    kv = SimpleNamespace(_act=torch.bfloat16, _device=torch.device("cpu"), head_dim=64, n_kv_heads=2, _ref=None,
+                         lib=SimpleNamespace(bz_op_paged_attention=attention))
+    batch = SimpleNamespace(T=3, handle=None)
+    good = dict(q=torch.zeros(3, 256, dtype=torch.bfloat16), out=torch.zeros(3, 256, dtype=torch.bfloat16),
+                rope=torch.zeros(8, 32, 2), workspace=torch.zeros(1024, dtype=torch.uint8))
+
+    def attend(**more):
+        args = dict(good, **more)
+        B.op_paged_attention(batch, kv, args.pop("q"), args.pop("out"), **args)
+
+    return attend, reached
+
+
+def test_workspaces_that_are_not_memory_on_the_device(call):
+    attend, reached = call
+    attend()
+    attend(workspace=None)
+    attend(workspace=torch.zeros(16, 16))                    # any type and shape, side by side
+    assert len(reached) == 3 and reached[0][-2] == 1024 and reached[2][-2] == 1024
+    space = torch.zeros(64, 64, dtype=torch.uint8)
+    for bad in (space.to("meta"), torch.zeros(1, dtype=torch.uint8).expand(1 << 20), space[:, ::2], space.t()):
+        with pytest.raises(ValueError):
+            attend(workspace=bad)
+    assert len(reached) == 3
