@@ -731,7 +731,9 @@ def _pitch(x) -> int:
 def _rope(kv: PagedKv, rope):
     if rope is None:
         return 0, 0
-    if rope.shape[1:] != (kv.head_dim // 2, 2) or not rope.is_contiguous() or rope.element_size() != 4 or rope.device != kv._device:
+    import torch
+    if (rope.shape[1:] != (kv.head_dim // 2, 2) or not rope.is_contiguous() or rope.dtype != torch.float32
+            or rope.device != kv._device):
         raise ValueError("rope must be a contiguous float32 tensor [positions, head_dim/2, 2] on the cache's device")
     return rope.data_ptr(), rope.shape[0]
 

@@ -42,3 +42,13 @@ def test_workspaces_that_are_not_memory_on_the_device(call):
         with pytest.raises(ValueError):
             attend(workspace=bad)
     assert len(reached) == 3
+
+
+def test_rotary_tables_of_another_type(call):
+    attend, reached = call
+    attend(rope=torch.zeros(8, 32, 2))
+    for bad in (torch.zeros(8, 32, 2, dtype=torch.int32), torch.zeros(8, 32, 2, dtype=torch.float64), torch.zeros(8, 32, 2).to("meta"),
+                torch.zeros(2, 8, 32).permute(1, 2, 0), torch.zeros(8, 64)):
+        with pytest.raises(ValueError):
+            attend(rope=bad)
+    assert len(reached) == 1
