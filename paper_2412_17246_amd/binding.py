@@ -693,8 +693,8 @@ class PagedKv:
         if not (k.is_cuda and k.device == v.device == page_table.device):
             raise ValueError("k, v and page_table must be on one GPU")
         page = page_size * n_kv_heads * head_dim
-        if page < 1 or k.numel() % page or k.numel() != v.numel():
-            raise ValueError("k and v must hold the same number of whole pages")
+        if page < 1 or k.numel() < page or k.numel() % page or k.numel() != v.numel():
+            raise ValueError("k and v must hold the same number of whole pages, one at least")
         self.k, self.v, self.page_table, self.fp32_debug = k, v, page_table, fp32_debug
         self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
         self.desc = bz_paged_kv(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), k.numel() // page, page_size,

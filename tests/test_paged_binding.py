@@ -52,3 +52,30 @@ def test_rotary_tables_of_another_type(call):
         with pytest.raises(ValueError):
             attend(rope=bad)
     assert len(reached) == 1
+
+
+class OnGpu:
+    """What PagedKv asks of a tensor."""
+
+    def __init__(self, shape, dtype):
+        self.t = torch.empty(shape, dtype=dtype, device="meta")
+        self.dtype, self.shape, self.is_cuda, self.device = dtype, self.t.shape, True, torch.device("cuda", 0)
+        for f in ("dim", "is_contiguous", "numel", "element_size"):
+            setattr(self, f, getattr(self.t, f))
+
+    def data_ptr(self):
+        return 4096
+
+
+@pytest.mark.parametrize("fp32", [False, True], ids=["bf16", "fp32dbg"])
+def test_a_cache_of_no_pages(fp32):
+    act = torch.float32 if fp32 else torch.bfloat16
+    table = OnGpu((2, 3), torch.int32)
+    make = lambda n, table=table: B.PagedKv(32, 2, 64, k=OnGpu((n, 2, 32 * 64), act), v=OnGpu((n, 2, 32 * 64), act),  # noqa: E731
+                                            page_table=table, fp32_debug=fp32)
+    assert make(1).desc.n_pages == 1
+    with pytest.raises(ValueError):
+        make(0)
+    for shape in ((0, 3), (2, 0)):                           # and of no rows, or none in a row
+        with pytest.raises(B.BzError):
+            make(1, OnGpu(shape, torch.int32))
