@@ -497,7 +497,9 @@ int bz_rope_table(int positions, int head_dim, float base, float* out);
  * as bz_rope_table writes it) keys are rotated on the way, element j with j + head_dim/2; NULL: they are stored as they are.
  * A rotated key and a value are rounded once, to the cache's type; in BZ_KV_E4M3 finite values and infinities beyond the largest
  * e4m3 number (448) are stored as that, NaN as NaN.  Positions that the batch does not append keep their contents.
- * BZ_EINVAL for a bad argument, BZ_ECAPACITY if a sequence outgrows its row of the table or the rotary table. */
+ * BZ_EINVAL for a bad argument, BZ_ECAPACITY if a sequence outgrows its row of the table or the rotary table, or if an operation here
+ * would take more workgroups than a launch can have (2^24: the attention of single tokens takes one per 256 positions and kv head;
+ * under a window, and for sequences of few new tokens, as many for each as for the longest of them). */
 int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void* k, int64_t k_stride, const void* v,
                        int64_t v_stride, const float* rope, int rope_positions, void* stream);
 

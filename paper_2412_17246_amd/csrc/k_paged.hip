@@ -225,16 +225,34 @@ static int heads_together(int64_t blocks, int Hkv, int par, int most) {
     return (h + par - 1) / par * par;
 }
 
+struct AppendGrid {
+    int heads_per_wg, hgroups, row_wgs;
+    int64_t block_wgs, all;
+};
+template <int D, bool E4M3>
+static AppendGrid append_grid(const BatchView& bv, const PagedView& kv) {
+    AppendGrid g;
+    const int64_t blocks = (int64_t)bv.n_prefill_items * kAppendBlocks;
+    g.heads_per_wg = heads_together(blocks, kv.Hkv, Blocks<D, E4M3>::PAR, 8);
+    g.hgroups = (kv.Hkv + g.heads_per_wg - 1) / g.heads_per_wg;
+    g.row_wgs = (kv.Hkv * (D / 16 + D / 8) + 255) / 256;
+    g.block_wgs = blocks * g.hgroups;
+    g.all = g.block_wgs + (int64_t)bv.n_decode * g.row_wgs;
+    return g;
+}
+static AppendGrid append_grid(bool e4m3, const BatchView& bv, const PagedView& kv) {
+    auto grid = kv.d == 128 ? (e4m3 ? append_grid<128, true> : append_grid<128, false>) : (e4m3 ? append_grid<64, true> : append_grid<64, false>);
+    return grid(bv, kv);
+}
+bool paged_append_fits(bool e4m3, const BatchView& bv, const PagedView& kv) { return append_grid(e4m3, bv, kv).all <= kMaxWorkgroups; }
+
 template <int D, bool E4M3>
 static void launch_append(const act_t* k, size_t k_stride, const act_t* v, size_t v_stride, const PagedRope& rope, const BatchView& bv,
                           const PagedView& kv, hipStream_t st) {
-    const int blocks = bv.n_prefill_items * kAppendBlocks;
-    const int hpw = heads_together(blocks, kv.Hkv, Blocks<D, E4M3>::PAR, 8), hgroups = (kv.Hkv + hpw - 1) / hpw;
-    const int row_wgs = (kv.Hkv * (D / 16 + D / 8) + 255) / 256;
-    const int grid = blocks * hgroups + bv.n_decode * row_wgs;
-    if (grid > 0)
-        hipLaunchKernelGGL((paged_append_kernel<D, E4M3>), dim3(grid), dim3(256), 0, st, k, k_stride, v, v_stride, rope, bv, kv, hpw,
-                           hgroups, blocks * hgroups, row_wgs);
+    const AppendGrid g = append_grid<D, E4M3>(bv, kv);
+    if (g.all > 0)
+        hipLaunchKernelGGL((paged_append_kernel<D, E4M3>), dim3((unsigned)g.all), dim3(256), 0, st, k, k_stride, v, v_stride, rope, bv, kv,
+                           g.heads_per_wg, g.hgroups, (int)g.block_wgs, g.row_wgs);
 }
 
 void launch_paged_append(const act_t* k, size_t k_stride, const act_t* v, size_t v_stride, const PagedRope& rope, bool e4m3,
@@ -303,11 +321,20 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedView kv, int row, 
     }
 }
 
+static int read_blocks(int pos0, int n) { return ((pos0 + n - 1) >> 5) - (pos0 >> 5) + 1; }
+
 template <int D, bool E4M3>
 static void launch_read(const PagedView& kv, int row, int pos0, int n, act_t* k, act_t* v, hipStream_t st) {
-    const int blocks = ((pos0 + n - 1) >> 5) - (pos0 >> 5) + 1;
+    const int blocks = read_blocks(pos0, n);
     const int hpw = heads_together(blocks, kv.Hkv, Blocks<D, E4M3>::PAR, 8), hgroups = (kv.Hkv + hpw - 1) / hpw;
     hipLaunchKernelGGL((paged_read_kernel<D, E4M3>), dim3(blocks * hgroups), dim3(256), 0, st, kv, row, pos0, n, k, v, hpw, hgroups);
+}
+
+bool paged_read_fits(bool e4m3, const PagedView& kv, int pos0, int n) {
+    const int64_t blocks = read_blocks(pos0, n);
+    const int par = kv.d == 128 ? (e4m3 ? Blocks<128, true>::PAR : Blocks<128, false>::PAR) : (e4m3 ? Blocks<64, true>::PAR : Blocks<64, false>::PAR);
+    const int hpw = heads_together(blocks, kv.Hkv, par, 8);
+    return blocks * ((kv.Hkv + hpw - 1) / hpw) <= kMaxWorkgroups;
 }
 
 void launch_paged_read(bool e4m3, const PagedView& kv, int row, int pos0, int n, act_t* k, act_t* v, hipStream_t st) {
@@ -344,6 +371,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const act_t* __restri
     }
 }
 
+bool paged_append_fits(bool, const BatchView& bv, const PagedView&) { return bv.T <= kMaxWorkgroups; }
+
 void launch_paged_append(const act_t* k, size_t k_stride, const act_t* v, size_t v_stride, const PagedRope& rope, bool e4m3,
                          const BatchView& bv, const PagedView& kv, hipStream_t st) {
     auto kern = e4m3 ? paged_append_kernel<true> : paged_append_kernel<false>;
@@ -363,6 +392,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedView kv, int row, 
         from_f32(v[(size_t)i * kv.Hkv * d + u], vx);
     }
 }
+
+bool paged_read_fits(bool, const PagedView&, int, int n) { return n <= kMaxWorkgroups; }
 
 void launch_paged_read(bool e4m3, const PagedView& kv, int row, int pos0, int n, act_t* k, act_t* v, hipStream_t st) {
     auto kern = e4m3 ? paged_read_kernel<true> : paged_read_kernel<false>;

@@ -924,13 +924,31 @@ size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, in
     return narrow_bytes(w, bv, Hq, d) + wide;
 }
 
+static int64_t narrow_grid(const PagedWork& w, const BatchView& bv, int Hkv) {
+    return (w.list + ((int64_t)bv.n_decode + w.n_short - w.first) * w.chunks) * Hkv * w.col_tiles;
+}
+static int64_t wide_grid(const PagedWork& w, const BatchView& bv, int Hq) {
+    return w.wide_units > 0 ? (int64_t)bv.n_prefill_items * Hq * w.splits : 0;
+}
+// tokens whose chunks are joined, and groups of 32 rows whose key ranges are
+static int64_t join_tokens(const PagedWork& w, const BatchView& bv) {
+    return w.max_chunks > 1 ? bv.n_decode + (int64_t)w.n_short * w.short_tokens : 0;
+}
+static int64_t join_rows(const PagedWork& w, const BatchView& bv) {
+    return w.wide_units > 0 && w.splits > 1 ? ((int64_t)bv.T * w.by_group.d + 31) / 32 : 0;
+}
+bool paged_attention_fits(const PagedWork& w, const BatchView& bv, int Hq, int Hkv) {
+    return narrow_grid(w, bv, Hkv) <= kMaxWorkgroups && wide_grid(w, bv, Hq) <= kMaxWorkgroups &&
+           join_tokens(w, bv) + join_rows(w, bv) <= kMaxWorkgroups && (int64_t)bv.T * w.by_group.d < 0x7fffff00LL;     // rows are ints
+}
+
 template <int D, bool E4M3, bool ROTATE, bool SPLIT>
 static void launch_wide(const PagedQuery& q, const PagedWork& w, const BatchView& bv, const PagedView& kv, float* ws, hipStream_t st) {
     constexpr int kLds = 2 * 4 * 32 * D * (int)sizeof(bf16);             // two stages of a K and a V tile
     static LdsLimit limit;
     (void)limit.raise(reinterpret_cast<const void*>(paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), kLds);
-    hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), dim3((unsigned)(bv.n_prefill_items * q.Hq * w.splits)), dim3(256), kLds, st, q,
-                       w, bv, kv, ws);
+    hipLaunchKernelGGL((paged_wide_kernel<D, E4M3, ROTATE, SPLIT>), dim3((unsigned)wide_grid(w, bv, q.Hq)), dim3(256), kLds, st, q, w, bv,
+                       kv, ws);
 }
 
 template <int D, bool E4M3>
@@ -940,7 +958,7 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
         // waves per SIMD: what the registers, and with 32 rows the LDS, leave room for; two for bf16 of d = 128, where a third
         // keeps the memory streams in shorter runs
         constexpr int FEW = E4M3 || D == 64 ? 4 : 2;
-        const unsigned grid = (unsigned)((w.list + (n_narrow - w.first) * w.chunks) * kv.Hkv * w.col_tiles);
+        const unsigned grid = (unsigned)narrow_grid(w, bv, kv.Hkv);
         auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, FEW> : paged_narrow_kernel<D, E4M3, kNarrowRows, 3>;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
     }
@@ -950,11 +968,10 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
                                : (w.splits > 1 ? launch_wide<D, E4M3, false, true> : launch_wide<D, E4M3, false, false>);
         rows(q, w, bv, kv, wide, st);
     }
-    const bool chunks = n_narrow > 0 && w.max_chunks > 1, ranges = w.wide_units > 0 && w.splits > 1;
+    const int tokens = (int)join_tokens(w, bv), rows32 = (int)join_rows(w, bv);
+    const bool chunks = tokens > 0, ranges = rows32 > 0;
     if (!chunks && !ranges) return;
     const int threads = ranges ? 256 : 128, heads = threads / (D / 4);       // of one workgroup
-    const int tokens = chunks ? bv.n_decode + w.n_short * w.short_tokens : 0;
-    const int rows32 = ranges ? (int)(((int64_t)bv.T * w.by_group.d + 31) / 32) : 0;
     const unsigned across = std::max(chunks ? (q.Hq + heads - 1) / heads : 0, ranges ? kv.Hkv : 0);
     auto join = chunks ? (ranges ? paged_join_kernel<D, true, true> : paged_join_kernel<D, true, false>) : paged_join_kernel<D, false, true>;
     hipLaunchKernelGGL(join, dim3(tokens + rows32, across), dim3(threads), 0, st, q, w, bv, kv, ws, wide, tokens);
@@ -1025,6 +1042,8 @@ __global__ __launch_bounds__(64) void paged_attn_plain_kernel(PagedQuery a, Batc
     for (int i = 0; i < D / 64; ++i)
         from_f32(a.out[(size_t)t * a.out_stride + h * D + lane + 64 * i], l > 0.f ? o[i] / l * kv.v_scale : 0.f);
 }
+
+bool paged_attention_fits(const PagedWork&, const BatchView&, int, int) { return true; }      // 64 threads per token
 
 size_t paged_attention_bytes(const PagedWork&, const BatchView&, int, int, int) { return 0; }
 

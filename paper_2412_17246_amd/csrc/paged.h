@@ -80,6 +80,10 @@ __device__ __forceinline__ void cache_put(void* base, size_t at, float x) {
     else from_f32(static_cast<act_t*>(base)[at], x);
 }
 
+// Whether a launch can have as many workgroups as an operation takes: the runtime counts a grid's threads in 32 bits.
+constexpr int64_t kMaxWorkgroups = 0xffffffffLL / 256;      // of 256 threads
+bool paged_append_fits(bool e4m3, const BatchView& bv, const PagedView& kv);
+bool paged_read_fits(bool e4m3, const PagedView& kv, int pos0, int n);
 void launch_paged_append(const act_t* k, size_t k_stride, const act_t* v, size_t v_stride, const PagedRope& rope, bool e4m3,
                          const BatchView& bv, const PagedView& kv, hipStream_t st);
 void launch_paged_read(bool e4m3, const PagedView& kv, int row, int pos0, int n, act_t* k, act_t* v, hipStream_t st);
@@ -130,6 +134,7 @@ struct PagedWork {
     int splits;
     Divisor by_heads, by_chunks, by_tiles, by_group;   // n_kv_heads * col_tiles, chunks, col_tiles, G
 };
+bool paged_attention_fits(const PagedWork& w, const BatchView& bv, int Hq, int Hkv);
 size_t paged_attention_bytes(const PagedWork& w, const BatchView& bv, int Hq, int Hkv, int d);
 void launch_paged_attention(const PagedQuery& q, const PagedWork& w, bool e4m3, const BatchView& bv, const PagedView& kv,
                             float* ws, hipStream_t st);

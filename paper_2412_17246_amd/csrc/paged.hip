@@ -92,7 +92,7 @@ PagedWork work_of(const bz_batch* b, const BatchView& bv, int Hq, int Hkv, int w
     int64_t units = 0, keys = 0;
     for (int s = 0; s < b->B; ++s) {
         const int n = b->q_start[s + 1] - b->q_start[s];
-        if (n < 2 || n * G <= w.narrow_limit) continue;
+        if (n < 2 || (int64_t)n * G <= w.narrow_limit) continue;
         const int64_t rows = (int64_t)n * G;
         units += (rows + kWideRows - 1) / kWideRows * Hkv;
         keys = std::max(keys, keys_of((int64_t)b->kv_before[s] + n - std::min<int64_t>(n, kWideRows / G + 1), std::min<int64_t>(n, kWideRows / G + 1), window));
@@ -152,6 +152,7 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
     hipStream_t st = (hipStream_t)stream;
     int rc = lengths_ok(batch, kv, rope, rope_positions);
     if (rc) return rc;
+    if (!paged_append_fits(kv->dtype == BZ_KV_E4M3, batch_view(batch), view_of(kv))) return BZ_ECAPACITY;
     rc = batch_before_run(batch, st);
     if (rc) return rc;
     launch_paged_append((const act_t*)k, (size_t)k_stride, (const act_t*)v, (size_t)v_stride, PagedRope{rope, rope_positions},
@@ -185,6 +186,7 @@ int bz_op_paged_attention(const bz_batch* batch, const bz_paged_kv* kv, const vo
     if (rc) return rc;
     const BatchView bv = batch_view(batch);
     const PagedWork work = work_of(batch, bv, n_q_heads, kv->n_kv_heads, window);
+    if (!paged_attention_fits(work, bv, n_q_heads, kv->n_kv_heads)) return BZ_ECAPACITY;
     const size_t need = paged_attention_bytes(work, bv, n_q_heads, kv->n_kv_heads, kv->head_dim);
     if (need && (!workspace || workspace_bytes < need)) return BZ_ENOMEM;
     rc = batch_before_run(batch, st);
@@ -209,6 +211,7 @@ int bz_op_paged_read(const bz_paged_kv* kv, int row, int pos0, int n, void* k, v
     if ((int64_t)pos0 + n > (int64_t)kv->pages_per_row * kv->page_size) return BZ_ECAPACITY;
     if (n == 0) return BZ_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return BZ_EINVAL;
+    if (!paged_read_fits(kv->dtype == BZ_KV_E4M3, view_of(kv), pos0, n)) return BZ_ECAPACITY;
     launch_paged_read(kv->dtype == BZ_KV_E4M3, view_of(kv), row, pos0, n, (act_t*)k, (act_t*)v, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? BZ_OK : hip_fail(e, "launch");

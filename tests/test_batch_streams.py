@@ -264,3 +264,48 @@ def test_a_change_outside_a_graph_that_is_being_captured(standin, fp32):
         assert hip.standin_dead_uses() == 0 and hip.standin_forbidden() == 0
 
     run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_grids_that_a_launch_cannot_have_are_refused(standin, fp32):
+    """The runtime counts a grid's threads in 32 bits; a number of workgroups beyond that wrapped round and left sequences out."""
+    def scenario():
+        import numpy as np
+        fp32 = bool(L.bz_build_info())
+        top = (1 << 32) // 256 - 1
+        def grid():
+            out = (C.c_uint32 * 3)()
+            hip.standin_grid(out)
+            return out[0], out[1], out[2]
+        def attend(b, kv, heads=2, window=0):
+            width = heads * kv.head_dim
+            return L.bz_op_paged_attention(b.handle, C.byref(kv), 4096, width, 8192, width, heads, 0.0, window, None, 0, 4096, 1 << 62, S)
+        def batch(n, q, before):
+            n_seqs = len(before)
+            return B.Batch(L, np.arange(n_seqs + 1) * q, np.arange(n_seqs), before)
+        def cache(rows, heads=2):
+            return B.bz_paged_kv(4096, 8192, 256, 64, 1024, rows, 1 << 19, heads, 64, B.BZ_KV_ACT, 1.0, 1.0)
+        # drafts beside one of 2^29 positions: sequences times the longest's chunks times kv heads
+        for n, rc in ((1001, ECAPACITY), (4, ECAPACITY), (3, 0)):  # 2^21 chunks and 2 heads: four are one workgroup too many
+            b = batch(n, 2, [(1 << 29) - 2] + [7] * (n - 1))
+            launches = hip.standin_launches()
+            got = attend(b, cache(n))
+            assert got == (0 if fp32 else rc), (n, got)          # the plain kernel has a workgroup per token and head
+            assert hip.standin_launches() - launches == (1 if fp32 else 0 if rc else 2)
+            assert attend(b, cache(n), window=100) == 0
+            b.close()
+        # 70000 sequences of two tokens, 32 rows each, on 1024 kv heads
+        b = batch(70000, 2, [0] * 70000)
+        assert append(b, S, cache(70000, 1024)) == (0 if fp32 else ECAPACITY)
+        assert append(b, S, cache(70000, 64)) == 0 and grid()[0] <= top
+        assert attend(b, cache(70000, 1024), 1024) == (0 if fp32 else ECAPACITY)
+        assert attend(b, cache(70000, 64), 64) == 0
+        b.close()
+        far = cache(1, 1024)
+        launches = hip.standin_launches()
+        far.pages_per_row = 1 << 20
+        assert L.bz_op_paged_read(C.byref(far), 0, 0, 1 << 30, 4096, 4096, S) == ECAPACITY
+        assert hip.standin_launches() == launches
+        assert L.bz_op_paged_read(C.byref(far), 0, 0, 1 << 20, 4096, 4096, S) == 0
+
+    run(standin, scenario, fp32)
