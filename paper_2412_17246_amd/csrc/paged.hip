@@ -152,11 +152,14 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
     hipStream_t st = (hipStream_t)stream;
     int rc = lengths_ok(batch, kv, rope, rope_positions);
     if (rc) return rc;
-    if (!paged_append_fits(kv->dtype == BZ_KV_E4M3, batch_view(batch), view_of(kv))) return BZ_ECAPACITY;
+    const BatchView bv = batch_view(batch);
+    const PagedView view = view_of(kv);
+    const bool e4m3 = kv->dtype == BZ_KV_E4M3;
+    if (!paged_append_fits(e4m3, bv, view)) return BZ_ECAPACITY;
     rc = batch_before_run(batch, st);
     if (rc) return rc;
     launch_paged_append((const act_t*)k, (size_t)k_stride, (const act_t*)v, (size_t)v_stride, PagedRope{rope, rope_positions},
-                        kv->dtype == BZ_KV_E4M3, batch_view(batch), view_of(kv), st);
+                        e4m3, bv, view, st);
     return launched(batch, st);
 } catch (...) {
     return BZ_ENOMEM;
