@@ -28,17 +28,22 @@ struct Blocks {
     }
 };
 
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(a), e4m3_range(b), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(c), e4m3_range(d), lo, true);
+// four numbers from x[i] on over the scale, as e4m3
+template <int VEC>
+__device__ __forceinline__ uint32_t pack4(const float (&x)[VEC], int i, float scale, float inv) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = e4m3_range(quotient(x[i + e], scale, inv));
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
 }
 // VEC numbers as the cache holds them
 template <bool E4M3, int VEC>
-__device__ __forceinline__ u32x4 pack(const float (&x)[VEC], float inv) {
+__device__ __forceinline__ u32x4 pack(const float (&x)[VEC], float scale, float inv) {
     if constexpr (E4M3) {
         u32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = pack4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
+        for (int i = 0; i < 4; ++i) r[i] = pack4(x, 4 * i, scale, inv);
         return r;
     } else {
         bf16x8 r;
@@ -123,15 +128,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const bf16* __restric
             const size_t at = block_base(kv, id, head, pos);
             if constexpr (E4M3) {
                 uint2 a, c;
-                a.x = pack4(lo[0] * kv.k_inv, lo[1] * kv.k_inv, lo[2] * kv.k_inv, lo[3] * kv.k_inv);
-                a.y = pack4(lo[4] * kv.k_inv, lo[5] * kv.k_inv, lo[6] * kv.k_inv, lo[7] * kv.k_inv);
-                c.x = pack4(hi[0] * kv.k_inv, hi[1] * kv.k_inv, hi[2] * kv.k_inv, hi[3] * kv.k_inv);
-                c.y = pack4(hi[4] * kv.k_inv, hi[5] * kv.k_inv, hi[6] * kv.k_inv, hi[7] * kv.k_inv);
+                a.x = pack4(lo, 0, kv.k_scale, kv.k_inv);
+                a.y = pack4(lo, 4, kv.k_scale, kv.k_inv);
+                c.x = pack4(hi, 0, kv.k_scale, kv.k_inv);
+                c.y = pack4(hi, 4, kv.k_scale, kv.k_inv);
                 *reinterpret_cast<uint2*>(kc + at + k_block_offset<true>(p, j)) = a;
                 *reinterpret_cast<uint2*>(kc + at + k_block_offset<true>(p, D / 2 + j)) = c;
             } else {
-                *reinterpret_cast<u32x4*>(kc + (at + k_block_offset<false>(p, j)) * 2) = pack<false>(lo, 1.f);
-                *reinterpret_cast<u32x4*>(kc + (at + k_block_offset<false>(p, D / 2 + j)) * 2) = pack<false>(hi, 1.f);
+                *reinterpret_cast<u32x4*>(kc + (at + k_block_offset<false>(p, j)) * 2) = pack<false>(lo, 1.f, 1.f);
+                *reinterpret_cast<u32x4*>(kc + (at + k_block_offset<false>(p, D / 2 + j)) * 2) = pack<false>(hi, 1.f, 1.f);
             }
         } else if ((unit -= Hkv * KU) < Hkv * VU) {
             // neighbouring threads have neighbouring head dims: a wave's store touches few lines
@@ -142,7 +147,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const bf16* __restric
             for (int e = 0; e < 8; ++e) x[e] = (float)src[e * VU];
             const size_t at = block_base(kv, id, head, pos);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cache_put<E4M3>(kv.v, at + v_block_offset<E4M3>(p, j + e * VU, D), E4M3 ? x[e] * kv.v_inv : x[e]);
+            for (int e = 0; e < 8; ++e) cache_put<E4M3>(kv.v, at + v_block_offset<E4M3>(p, j + e * VU, D), E4M3 ? quotient(x[e], kv.v_scale, kv.v_inv) : x[e]);
         }
         return;
     }
@@ -184,8 +189,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const bf16* __restric
         if (cs) rotate(lo, hi, cs);
         uint8_t* kd = kc + base + h * head_bytes + kp * 16;
         if (k_in) {
-            *reinterpret_cast<u32x4*>(kd + unit * 512) = pack<E4M3>(lo, kv.k_inv);
-            *reinterpret_cast<u32x4*>(kd + (unit + B::UNITS) * 512) = pack<E4M3>(hi, kv.k_inv);
+            *reinterpret_cast<u32x4*>(kd + unit * 512) = pack<E4M3>(lo, kv.k_scale, kv.k_inv);
+            *reinterpret_cast<u32x4*>(kd + (unit + B::UNITS) * 512) = pack<E4M3>(hi, kv.k_scale, kv.k_inv);
         }
         float x[B::VEC], y[B::VEC];
         bool all = true;
@@ -196,7 +201,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const bf16* __restric
             const int pe = first + B::v_pos(w, e);
             all &= pe >= p_lo && pe < p_hi;
         }
-        const u32x4 px = pack<E4M3>(x, kv.v_inv), py = pack<E4M3>(y, kv.v_inv);
+        const u32x4 px = pack<E4M3>(x, kv.v_scale, kv.v_inv), py = pack<E4M3>(y, kv.v_scale, kv.v_inv);
         uint8_t* vd = vc + base + h * head_bytes + (w * D + j) * 16;
         if (all) {
             *reinterpret_cast<u32x4*>(vd) = px;
@@ -361,13 +366,13 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const act_t* __restri
         const float lo = to_f32(kr[head * d + j]), hi = to_f32(kr[head * d + half + j]);
         const float c = cs ? cs[2 * j] : 1.f, sn = cs ? cs[2 * j + 1] : 0.f;
         const float o_lo = cs ? lo * c - hi * sn : lo, o_hi = cs ? hi * c + lo * sn : hi;
-        cache_put<E4M3>(kv.k, at + k_block_offset<E4M3>(p, j), E4M3 ? o_lo * kv.k_inv : o_lo);
-        cache_put<E4M3>(kv.k, at + k_block_offset<E4M3>(p, half + j), E4M3 ? o_hi * kv.k_inv : o_hi);
+        cache_put<E4M3>(kv.k, at + k_block_offset<E4M3>(p, j), E4M3 ? quotient(o_lo, kv.k_scale, kv.k_inv) : o_lo);
+        cache_put<E4M3>(kv.k, at + k_block_offset<E4M3>(p, half + j), E4M3 ? quotient(o_hi, kv.k_scale, kv.k_inv) : o_hi);
     }
     for (int u = threadIdx.x; u < kv.Hkv * d; u += 256) {
         const int head = u / d, j = u - head * d;
         const float x = to_f32(vr[u]);
-        cache_put<E4M3>(kv.v, block_base(kv, id, head, pos) + v_block_offset<E4M3>(p, j, d), E4M3 ? x * kv.v_inv : x);
+        cache_put<E4M3>(kv.v, block_base(kv, id, head, pos) + v_block_offset<E4M3>(p, j, d), E4M3 ? quotient(x, kv.v_scale, kv.v_inv) : x);
     }
 }
 

@@ -19,7 +19,7 @@ struct PagedView {
     int n_pages, per_row, page_shift;
     int Hkv, d;
     float k_scale, v_scale;    // what 1 in the cache stands for
-    float k_inv, v_inv;        // and what the append multiplies by
+    float k_inv, v_inv;        // their reciprocals
 };
 
 struct PagedRope {
@@ -58,6 +58,16 @@ __device__ __forceinline__ const float* rope_row(const PagedRope& rope, int pos,
     return rope.tab + (size_t)(pos < rope.positions ? pos : rope.positions - 1) * d;
 }
 
+// x / scale, given the scale's reciprocal, rounded to the odd one of the two floats around it: rounding that to e4m3 is rounding the
+// quotient itself.  The product with the reciprocal can be off by a step, which makes a tie between two e4m3 numbers none (87.5 / 7 is
+// 12.5, times 1/7 more); with what is left over, exact in the multiply-add, times the reciprocal it is the nearest float, and the sign of
+// what is left then says on which side the quotient lies.  Beyond the largest e4m3 number, and for zeros with their sign, the product
+// will do.
+__device__ __forceinline__ float quotient(float x, float scale, float inv) {
+    const float y = x * inv, q = fmaf(fmaf(-y, scale, x), inv, y), left = fmaf(-q, scale, x);
+    const int bits = __float_as_int(q), step = (bits & 1) || left == 0.f ? 0 : (__float_as_int(left) ^ bits) < 0 ? -1 : 1;
+    return y != 0.f && fabsf(y) < 2.f * kE4m3Max ? __int_as_float(bits + step) : y;
+}
 // Saturates to the largest e4m3 number; NaN stays.
 __device__ __forceinline__ float e4m3_range(float x) {
     const float c = fminf(fmaxf(x, -kE4m3Max), kE4m3Max);

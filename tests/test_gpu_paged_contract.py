@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import paged as P
-from tests.test_gpu_paged import CACHES, World
+from tests.test_gpu_paged import BUILDS, CACHES, World
 
 pytestmark = pytest.mark.gpu
 
@@ -46,6 +46,37 @@ def test_destroy_while_a_stream_that_ran_the_batch_is_captured(torch):
     assert torch.all(x == 1) and torch.equal(out, want) and torch.any(want != 0)
     batch.close()
     assert batch.handle is None
+
+
+def as_e4m3(x):
+    """The e4m3 number next to each of x (float64), ties to the even one, beyond the largest that."""
+    x = np.clip(x, -448, 448)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        e = np.maximum(np.floor(np.log2(np.abs(x))), -6)
+        step = 2.0 ** (e - 3)
+        return np.where(x == 0, 0.0, np.round(x / step) * step)      # numpy rounds halves to even
+
+
+@BUILDS
+@pytest.mark.parametrize("prompt", [False, True], ids=["single", "prompt"])
+@pytest.mark.parametrize("scale", [7.0, 0.875, 0.0137, 0.1, 3.0, 2.0 ** -20, 1e30])
+def test_e4m3_append_rounds_the_quotient_once(torch, fp32, prompt, scale):
+    """Every bf16 number over a scale: the e4m3 number next to the exact quotient.  A tie is one only if the division says so: times
+    the scale's reciprocal, 87.5 / 7 is more than 12.5 and would go up."""
+    n = 128
+    seqs = [(n, 0)] if prompt else [(1, 31 + i % 3) for i in range(n)]
+    w = World(torch, seqs, 8, 8, 64, 64, fp32=fp32, e4m3=True, rope=False, scales=(scale, scale), seed=84)
+    bits = np.arange(65536, dtype=np.uint32).reshape(n, 512)
+    x = (bits << 16).view(np.float32)
+    dev = torch.from_numpy(x.copy()).cuda().to(w.act)
+    w.k, w.v = dev, dev.clone()
+    w.append()
+    with np.errstate(all="ignore"):
+        want = as_e4m3(x.astype(np.float64) / np.float64(np.float32(scale))).reshape(n, 8, 64)
+    got_k, got_v = w.download(w.dk), w.download(w.dv)
+    for i, (s, pos) in enumerate([(0, p) for p in range(n)] if prompt else [(s, b) for s, (_, b) in enumerate(seqs)]):
+        kp, vp = P.places(w.table[s], [pos], 8, 64, 64, 16)
+        assert np.array_equal(got_k[kp][0], want[i], equal_nan=True) and np.array_equal(got_v[vp][0], want[i], equal_nan=True), i
 
 
 @CACHES
