@@ -409,11 +409,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
-                sacc[b][r] = p;
-                l += p;
-            }
+            for (int r = 0; r < 16; ++r) sacc[b][r] = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -421,6 +417,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
                 bf16x8 pf;
 #pragma unroll
                 for (int x = 0; x < 8; ++x) pf[x] = (bf16)sacc[b][8 * t + x];
+#pragma unroll
+                for (int x = 0; x < 8; x += 2) l = add_pair(bf16x2{pf[x], pf[x + 1]}, l);    // of the weights as the product will use them
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
                     bf16x8 vv;

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import paged as P
+from tests import _util as U
 from tests.test_gpu_paged import BUILDS, CACHES, World
 
 pytestmark = pytest.mark.gpu
@@ -77,6 +78,32 @@ def test_e4m3_append_rounds_the_quotient_once(torch, fp32, prompt, scale):
     for i, (s, pos) in enumerate([(0, p) for p in range(n)] if prompt else [(s, b) for s, (_, b) in enumerate(seqs)]):
         kp, vp = P.places(w.table[s], [pos], 8, 64, 64, 16)
         assert np.array_equal(got_k[kp][0], want[i], equal_nan=True) and np.array_equal(got_v[vp][0], want[i], equal_nan=True), i
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("seqs", [[(1, 1 + i % 6) for i in range(64)], [(1, 520), (1, 1), (1, 300), (1, 2)], [(4, i % 5) for i in range(24)],
+                                  [(5, 300), (3, 600), (2, 0)], [(20, 0), (33, 1), (150, 4)]], ids=["single", "chunks", "drafts", "draft_chunks", "wide"])
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2), (16, 2)], ids=lambda h: "x".join(map(str, h)))
+def test_weights_are_summed_as_they_are_multiplied(torch, d, seqs, heads):
+    """Values that are the same at every position come back as they are, whatever the weights are rounded to: numerator and denominator
+    hold the same weights."""
+    v_scale = 0.0121
+    w = World(torch, seqs, *heads, d, 64, e4m3=True, scales=(0.02, v_scale), seed=85)
+    w.write_new()
+    # per head dim one e4m3 number whose product with the scale is far from the middle between two bf16 numbers: nearer to it than
+    # that come only sums of 600 positions in fp32, twice, and three roundings more, 1203 * 2^-24 < 2^-13
+    c = np.array([m * 2.0 ** e for e in (-3, 0, 4) for m in range(8, 16)]) * np.float64(np.float32(v_scale))
+    near = U.f64(U.W.bf16_bits_from_f32(c.astype(np.float32)))
+    step = 2.0 ** (np.floor(np.log2(c)) - 7)
+    ok = np.abs(np.abs(c - near) - step / 2) > 2.0 ** -13 * c
+    per_dim = np.resize((c / np.float64(np.float32(v_scale)))[ok], d)
+    want = np.resize(near[ok], d)
+    for s, (n, before) in enumerate(w.seqs):
+        _, vp = P.places(w.table[s], np.arange(n + before), heads[1], 64, d, 16)
+        w.hv[vp] = np.round(per_dim * 2 ** 10) / 2 ** 10
+    w.dv.copy_(w.upload(w.hv))
+    got = w.download(w.attend()).reshape(w.T, heads[0], d)
+    assert np.array_equal(got, np.broadcast_to(want, got.shape)), np.max(np.abs(got / want - 1))
 
 
 @CACHES
