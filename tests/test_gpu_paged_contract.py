@@ -5,7 +5,7 @@ import pytest
 
 from oracle import paged as P
 from tests import _util as U
-from tests.test_gpu_paged import BUILDS, CACHES, World
+from tests.test_gpu_paged import BUILDS, CACHES, HALF_BF16, HALF_F32, World
 
 pytestmark = pytest.mark.gpu
 
@@ -104,6 +104,51 @@ def test_weights_are_summed_as_they_are_multiplied(torch, d, seqs, heads):
     w.dv.copy_(w.upload(w.hv))
     got = w.download(w.attend()).reshape(w.T, heads[0], d)
     assert np.array_equal(got, np.broadcast_to(want, got.shape)), np.max(np.abs(got / want - 1))
+
+
+@CACHES
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2), (8, 1)], ids=lambda h: "x".join(map(str, h)))
+@pytest.mark.parametrize("seqs", [[(1, 90), (1, 300), (1, 31), (1, 700)], [(4, 200), (3, 40), (2, 513)], [(64, 130), (150, 0)]],
+                         ids=["single", "draft", "wide"])
+def test_rotated_queries_keep_their_bits(torch, e4m3, d, heads, seqs):
+    """Scores so large that the queries' rounding decides: rotated queries are two bf16 whose sum is off by 2^-16, in the wide
+    kernel over e4m3 fp16, off by 2^-11, with weights as precise.  Queries of one bf16 would not pass: two parts by the bound of the
+    worst element, fp16 by the rms of all of them."""
+    wide = seqs[0][0] > 32
+    w = World(torch, seqs, *heads, d, 64, e4m3=e4m3, amplitude=3.0, scales=(0.05, 0.05), seed=86)
+    w.write_new()
+    got = w.download(w.attend()).reshape(w.T, heads[0], d)
+    half = 2.0 ** -11 if wide and e4m3 else HALF_BF16
+    worst = worst_of_one = 0.0
+    squares = np.zeros(4)                                    # of the error, of the error with queries of one bf16, of output and values
+    for s, (n, before) in enumerate(seqs):
+        a, b = w.q_start[s], w.q_start[s + 1]
+        pos = before + np.arange(n)
+        x = w.qkv64[a:b, :heads[0] * d].reshape(n, heads[0], d)
+        q = P.rotate(x, pos, w.rope64)
+        k, v, there = w.sequence(s)
+        want, moved = P.attention(q, k, v, pos, there, d ** -0.5)
+        sums = (len(there) + d) * HALF_F32 * 2
+        # three fp32 roundings in a rotated element, of terms up to its pair's length: 2^-21 of the pair's two
+        eps_q = (2.0 ** -11 if wide and e4m3 else HALF_BF16 ** 2) + 2.0 ** -21 + sums
+        # fp16 weights below 2^-20 of the largest are off by up to 2^-31 of it each
+        thin = len(there) * 2.0 ** -31 * np.max(np.abs(v)) if wide and e4m3 else 0.0
+        # weights in numerator and denominator move the output by half * sum w |v - out|, at most half * (sum w |v| + |out|)
+        tol = (HALF_BF16 + half) * np.abs(want) + moved(eps_q, half + sums) * (1 + 2 ** -4) + thin
+        worst = max(worst, np.max(np.abs(got[a:b] - want) / tol))
+        one = U.f64(U.W.bf16_bits_from_f32(q.astype(np.float32)))
+        off = P.attention(one, k, v, pos, there, d ** -0.5)[0] - want
+        worst_of_one = max(worst_of_one, np.max(np.abs(off) / tol))
+        squares += [want.size * np.mean(x ** 2) for x in (got[a:b] - want, off, want, v)]
+    assert worst <= 1, worst
+    if not (wide and e4m3):
+        assert worst_of_one > 1, worst_of_one                # the test can tell
+        return
+    # an eighth of the error of one bf16, the output's rounding and twice the weights', evenly spread: half / sqrt(3) each
+    rms, rms_of_one, rms_out, rms_v = np.sqrt(squares / (w.T * heads[0] * d))
+    bound = rms_of_one / 8 + (HALF_BF16 * rms_out + 2 * half * rms_v) / np.sqrt(3)
+    assert rms <= bound and bound < rms_of_one, (rms, bound, rms_of_one)
 
 
 @CACHES
