@@ -511,9 +511,10 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  * 8; pointers 16-byte aligned); out may be q itself, with the same stride.  Rows of out behind the last sequence are left alone.
  * `rope`: as above, queries are rotated as they are read; NULL: they are rotated already, or there is no rotation.
  * Softmax and sums are float.  Rounded (not in the fp32 debug build) are the weights, to bf16 for the product with the values, and a
- * rotated query, for the product with the keys, to two bf16 whose sum it is.  Over BZ_KV_E4M3, in sequences whose new tokens times
- * n_q_heads / n_kv_heads exceed 32, weights and queries are fp16 instead: 11 bits, and elements of a query below 2^-38 of its
- * largest count as nothing.
+ * rotated query, for the product with the keys, to two bf16 whose sum it is; the sum that divides is that of the rounded weights.
+ * Over BZ_KV_E4M3, in sequences whose new tokens times n_q_heads / n_kv_heads exceed 32, weights and queries are fp16 instead: 11
+ * bits, fewer for weights below 2^-20 of a query's largest and for elements of a query below 2^-27 of its largest, and below 2^-30
+ * and 2^-38 they may count as nothing.
  * A value that is not finite shows in every query that sees it, and may show in other queries of the same sequence and call:
  * those before it, and with a window those that have left it behind.  It does in no other sequence, nor in a call none of whose
  * queries sees it.  A key that is not finite shows in the queries that see it alone.
