@@ -510,11 +510,12 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  * q and out hold n_q_heads * head_dim activation elements per packed row, rows q_stride and out_stride elements apart (multiples of
  * 8; pointers 16-byte aligned); out may be q itself, with the same stride.  Rows of out behind the last sequence are left alone.
  * `rope`: as above, queries are rotated as they are read; NULL: they are rotated already, or there is no rotation.
- * Softmax and sums are float.  Rounded (not in the fp32 debug build) are the weights, to bf16 for the product with the values, and a
- * rotated query, for the product with the keys, to two bf16 whose sum it is; the sum that divides is that of the rounded weights.
- * Over BZ_KV_E4M3, in sequences whose new tokens times n_q_heads / n_kv_heads exceed 32, weights and queries are fp16 instead: 11
- * bits, fewer for weights below 2^-20 of a query's largest and for elements of a query below 2^-27 of its largest, and below 2^-30
- * and 2^-38 they may count as nothing.
+ * Softmax and sums are float.  Rounded (not in the fp32 debug build) are the operands of the products, and the sum that divides is that
+ * of the rounded weights.  In single tokens and sequences whose new tokens times n_q_heads / n_kv_heads are at most 32, a rotated query
+ * has 16 bits and a weight 15, over BZ_KV_E4M3 11 where those rows exceed eight.  In longer ones a rotated query has 16 bits and a weight
+ * is bf16; over BZ_KV_E4M3 both are fp16 there: 11 bits, fewer for weights below 2^-20 of a query's largest and for elements of a
+ * query below 2^-27 of its largest, and below 2^-30 and 2^-38 they may count as nothing.  (Lent memory with no room for a batch's
+ * list of short sequences makes long ones of them.)
  * A value that is not finite shows in every query that sees it, and may show in other queries of the same sequence and call:
  * those before it, and with a window those that have left it behind.  It does in no other sequence, nor in a call none of whose
  * queries sees it.  A key that is not finite shows in the queries that see it alone.

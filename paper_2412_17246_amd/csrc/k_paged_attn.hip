@@ -163,6 +163,13 @@ struct RowSoftmax {
     }
 };
 
+// the part of a number that `mask`, 16 bits or none, leaves of it
+__device__ __forceinline__ float above(float x, uint32_t mask) { return __uint_as_float(__float_as_uint(x) & mask); }
+// two numbers as bf16, cut off: what is cut is `x - above(x, 0xffff0000)`, exactly
+__device__ __forceinline__ bf16x2 upper_halves(float x, float y) {
+    return __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u));
+}
+
 // x of the lane plus x of the lane eight further in its row of sixteen
 __device__ __forceinline__ float add_eighth(float x) {
     return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, true));
@@ -189,11 +196,12 @@ __device__ __forceinline__ float2* partial_sums(float* partial, const PagedWork&
 // LDS in wave order.  Bound by the cache's bytes (64 sequences of up to 4096 positions on 8 kv heads with four query heads each, bf16:
 // 95.5 us, 5.8 TB/s; a streaming read has 7.1 at best), in few workgroups by one's 6.5 us from launch to end.
 //
-// Queries are kept as the sum of two bf16, rounded after the rotation to 16 bits and not to 8: what the matrix pipe does beside the
-// stream costs little.  With up to eight rows the second parts are columns 8..15, which the first parts leave free, and the scores'
-// two parts are added across lanes; with more they are products of their own.  The output's distance from a computation in 64 bits is
-// 2.1e-3 that way (rms, bf16's own rounding of the output 1.7e-3), against 2.7e-3 with queries of one bf16; the rest is the weights,
-// which are rounded to bf16 for the product.
+// Queries are kept as the sum of two bf16, rounded after the rotation to 16 bits and not to 8, and so are weights, cut off behind 15 or 16:
+// what the matrix pipe does beside the stream costs little.  With up to eight rows the second parts are columns 8..15, which the first
+// parts leave free, and two columns' scores, outputs and sums are added across lanes.  With more they are products of their own (24
+// drafts 47.8 -> 48.2 us a call); over e4m3, where that costs 6 %, weights are fp16 instead, 11 bits down to 2^-28 of the largest.  The
+// output's distance from a computation in 64 bits is 1.7e-3 (rms), which is its own rounding to bf16; with weights of one bf16 it was 2.1e-3,
+// with queries of one, too, 2.7e-3.
 //
 // A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d cache elements: a sixteenth of the bytes
 // for eight rows of e4m3.  Chunks of twice the length halve that and gain nothing (32 sequences of up to 12000 positions on 8 kv heads
@@ -326,6 +334,10 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
         for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
     // columns past the rows repeat the first and are dropped
     constexpr bool BESIDE = RT == 8;                         // second parts in columns of their own
+    // weights: two bf16; over e4m3 without room beside, fp16, from 2^14 down, which is exact in that as well
+    constexpr bool HALF = E4M3 && !BESIDE;
+    using P2 = typename std::conditional<HALF, f16x2, bf16x2>::type;
+    using P8 = typename std::conditional<HALF, f16x8, bf16x8>::type;
     const int col = BESIDE ? lq & 7 : lq, qr = col < rows ? col : 0;
     const bf16* qcol = &qs[BESIDE ? (lq >> 3) & 1 : 0][qr][0];
     if (live) {
@@ -404,29 +416,52 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[b][r]);
-        m = pair_max(mx) * a.scale_log2;                 // scale > 0
+        m = pair_max(mx) * a.scale_log2 - (HALF ? 14.f : 0.f);      // scale > 0
         const float ref = finite_or_0(m);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sacc[b][r] = exp2_flush(fmaf(sacc[b][r], a.scale_log2, -ref));
+        // columns 8..15 take the second parts of the weights, as they did of the queries
+        const uint32_t second = lq & 8 ? 0xffff0000u : 0;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                bf16x8 pf;
+                P8 pf, pl;
 #pragma unroll
-                for (int x = 0; x < 8; ++x) pf[x] = (bf16)sacc[b][8 * t + x];
-#pragma unroll
-                for (int x = 0; x < 8; x += 2) l = add_pair(bf16x2{pf[x], pf[x + 1]}, l);    // of the weights as the product will use them
+                for (int x = 0; x < 8; x += 2) {
+                    const float y = sacc[b][8 * t + x], z = sacc[b][8 * t + x + 1];
+                    P2 p;                                    // l: of the weights as the product will use them
+                    if constexpr (HALF) p = P2{(_Float16)y, (_Float16)z};
+                    else p = BESIDE ? upper_halves(y - above(y, second), z - above(z, second)) : upper_halves(y, z);
+                    l = add_pair(p, l);
+                    pf[x] = p[0];
+                    pf[x + 1] = p[1];
+                    if constexpr (!HALF && !BESIDE) {
+                        const P2 r = upper_halves(y - above(y, 0xffff0000u), z - above(z, 0xffff0000u));
+                        l = add_pair(r, l);
+                        pl[x] = r[0];
+                        pl[x + 1] = r[1];
+                    }
+                }
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
-                    bf16x8 vv;
-                    if (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
+                    P8 vv;
+                    if constexpr (HALF) vv = e4m3_to_f16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
+                    else if constexpr (E4M3) vv = e4m3_to_bf16(vf[b][db][2 * t], vf[b][db][2 * t + 1]);
                     else vv = *reinterpret_cast<const bf16x8*>(&vf[b][t * DB + db]);
-                    oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pf, oacc[db], 0, 0, 0);
+                    oacc[db] = product(vv, pf, oacc[db]);
+                    if constexpr (!HALF && !BESIDE) oacc[db] = product(vv, pl, oacc[db]);
                 }
             }
+        if (BESIDE) {
+            l = add_eighth(l);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) oacc[db][r] = add_eighth(oacc[db][r]);
+        }
         l = pair_sum(l);
     }
     // a wave that had nothing leaves m = -inf, l = 0, o = 0

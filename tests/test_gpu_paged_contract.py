@@ -184,3 +184,41 @@ def test_a_value_that_is_not_finite_under_a_window(torch, e4m3, heads, n):
     got = w.attend(window=window)                            # a key reaches those that see it alone
     same = torch.eq(got.view(torch.int16), want.view(torch.int16)).all(dim=1)
     assert torch.all(same[:a]) and torch.all(same[b:]) and torch.equal(same[a:b], ~sees) and torch.isnan(got[a:b][sees]).all()
+
+
+def of_bits(x, bits):
+    """x rounded to so many significant bits."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.round(m * 2.0 ** bits), e - bits)
+
+
+@CACHES
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2), (16, 2), (16, 1)], ids=lambda h: "x".join(map(str, h)))
+@pytest.mark.parametrize("seqs", [[(1, 90), (1, 300), (1, 31), (1, 700)] * 4, [(2, 200), (2, 40), (2, 513)] * 3], ids=["single", "draft"])
+def test_weights_of_short_sequences_keep_their_bits(torch, e4m3, d, heads, seqs):
+    """Weights of 15 bits, over e4m3 with more than eight rows of 11, and an output rounded to bf16: the rms of all errors is that of
+    an oracle with just these roundings, nearer to it than to one whose weights are bf16."""
+    w = World(torch, seqs, *heads, d, 64, e4m3=e4m3, seed=88)
+    w.write_new()
+    got = w.download(w.attend()).reshape(w.T, heads[0], d)
+    G = heads[0] // heads[1]
+    bits = 11 if e4m3 and max(n for n, _ in seqs) * G > 8 else 15
+    err, as_stated, as_bf16 = [], [], []
+    for s, (n, before) in enumerate(seqs):
+        a, b = w.q_start[s], w.q_start[s + 1]
+        pos = before + np.arange(n)
+        q = P.rotate(w.qkv64[a:b, :heads[0] * d].reshape(n, heads[0], d), pos, w.rope64)
+        k, v, _ = w.sequence(s)
+        for h in range(heads[0]):
+            score = np.where(np.arange(n + before) <= pos[:, None], q[:, h] @ k[:, h // G].T * d ** -0.5, -np.inf)
+            weight = np.exp(score - score.max(axis=1, keepdims=True))
+            out = lambda x: x @ v[:, h // G] / x.sum(axis=1, keepdims=True)  # noqa: E731
+            stored = lambda x: U.f64(U.W.bf16_bits_from_f32(x.astype(np.float32)))  # noqa: E731
+            want = out(weight)
+            err.append(got[a:b, h] - want)
+            as_stated.append(stored(out(of_bits(weight, bits))) - want)
+            as_bf16.append(stored(out(of_bits(weight, 8))) - want)
+    rms, stated, bf16 = (np.sqrt(np.mean(np.concatenate(x) ** 2)) for x in (err, as_stated, as_bf16))
+    assert stated * 1.1 < bf16                               # the test can tell
+    assert rms <= (stated + bf16) / 2, (rms, stated, bf16)
