@@ -520,7 +520,9 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  * those before it, and with a window those that have left it behind.  It does in no other sequence, nor in a call none of whose
  * queries sees it.  A key that is not finite shows in the queries that see it alone.
  * `workspace`: device scratch, 16-byte aligned, of at least bz_op_paged_attention_workspace_bytes() bytes for the same batch,
- * shapes and window (BZ_ENOMEM if smaller); calls that may overlap in time need workspaces of their own.
+ * shapes and window (BZ_ENOMEM if smaller); calls that may overlap in time need workspaces of their own.  It grows with the single
+ * tokens and the short sequences' new tokens, times query heads, times 256-position chunks of the longest of these sequences: one very
+ * long sequence among many short ones is better in a batch of its own.
  * Results depend within rounding on the other sequences of the batch, whose lengths say how key ranges are cut; the same call
  * gives the same bits every time.
  *

@@ -96,8 +96,8 @@ __device__ __forceinline__ void rotate(float (&lo)[VEC], float (&hi)[VEC], const
 // ---------------------------------------------------------------------------------------------
 // Append.  Sequences with several new tokens: one workgroup per block of 32 positions and `heads_per_wg` heads.  Single new tokens:
 // workgroups from `block_wgs` on, `row_wgs` per token, a thread per 8 rotation pairs or 8 values.  Bound by bytes, each moved once
-// (12000 tokens on 40 kv heads, bf16: 97 us, 4.0 TB/s, where a large copy has 4.7); a single token by the launch (2.3 us), many by the
-// lines that they touch: a value is one element of each of d pieces of 16 bytes (161 tokens on 32 heads, e4m3: 6.4 us for 10.5 MB of lines
+// (9378 tokens on 40 kv heads, bf16: 96 us, 4.1 TB/s, where a large copy has 4.7); a single token by the launch (2.1 us), many by the
+// lines that they touch: a value is one element of each of d pieces of 16 bytes (161 tokens on 32 heads, e4m3: 6.6 us for 10.5 MB of lines
 // in which 0.66 MB change; with eight neighbouring head dims to a thread, every store 64 lines, 8.9).
 // ---------------------------------------------------------------------------------------------
 constexpr int kAppendBlocks = kPrefillTileQ / 32 + 1;        // blocks that 128 tokens may touch

@@ -194,18 +194,19 @@ __device__ __forceinline__ float2* partial_sums(float* partial, const PagedWork&
 // positions, with all their loads in flight at once, and computes S = K Q^T and O = V^T P^T with 32x32x16 products whose
 // row operand is the cache as it lies in memory; rows of the problem are the 32 columns.  The four waves' results are merged through
 // LDS in wave order.  Bound by the cache's bytes (64 sequences of up to 4096 positions on 8 kv heads with four query heads each, bf16:
-// 95.5 us, 5.8 TB/s; a streaming read has 7.1 at best), in few workgroups by one's 6.5 us from launch to end.
+// 95.5 us, 5.8 TB/s; a streaming read has 7.1 at best), in few workgroups by one's 6.6 us from launch to end.
 //
 // Queries are kept as the sum of two bf16, rounded after the rotation to 16 bits and not to 8, and so are weights, cut off behind 15 or 16:
 // what the matrix pipe does beside the stream costs little.  With up to eight rows the second parts are columns 8..15, which the first
-// parts leave free, and two columns' scores, outputs and sums are added across lanes.  With more they are products of their own (24
-// drafts 47.8 -> 48.2 us a call); over e4m3, where that costs 6 %, weights are fp16 instead, 11 bits down to 2^-28 of the largest.  The
+// parts leave free, and two columns' scores, outputs and sums are added across lanes (of weights: 32 sequences on e4m3 80.4 -> 80.8 us a
+// call, 64 on bf16 99.8 both).  With more they are products of their own (of weights: 24 drafts 47.8 -> 48.2); over e4m3, where that costs
+// 6 %, weights are fp16 instead, 11 bits down to 2^-28 of the largest.  The
 // output's distance from a computation in 64 bits is 1.7e-3 (rms), which is its own rounding to bf16; with weights of one bf16 it was 2.1e-3,
 // with queries of one, too, 2.7e-3.
 //
 // A chunk's partial results are written and read once more, RT * (d + 2) floats for 512 * d cache elements: a sixteenth of the bytes
 // for eight rows of e4m3.  Chunks of twice the length halve that and gain nothing (32 sequences of up to 12000 positions on 8 kv heads
-// with eight query heads each, kernel and join: 81.3 us with one step of 64 positions per wave and four waves per SIMD, 83.8 with two
+// with eight query heads each, kernel and join, weights of one bf16: 81.3 us with one step of 64 positions per wave and four waves per SIMD, 83.8 with two
 // steps and the three waves that these leave room for).
 template <int D, bool E4M3, int RT, int WAVES>
 __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(256) void paged_narrow_kernel(
@@ -523,7 +524,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) __launch_bounds__(
 // an e4m3 cache, which fp16 holds exactly, by queries and weights in fp16, a query's row brought to fp16's range by a power of two
 // that its scores give back.  Distance of the output from a computation in 64 bits, rms: 2.0e-3 to 2.3e-3 over bf16 and 1.7e-3, the
 // output's own rounding, over e4m3.  With rotated queries in one bf16 it is 2.5e-3 to 2.9e-3, and the 48 products per tile and wave are
-// 32 (four prompts of 2048 tokens on 8 kv heads with eight query heads each: 305 us, with two 381).
+// 32 (four prompts of 2048 tokens on 8 kv heads with eight query heads each: 299 us, with two 375).
 //
 // Bound by the matrix pipe: those 48 products of random numbers take 1.2 us at the clock that the chip's power allows (25 ns each and
 // SIMD, registers only), a tile 1.4 per CU.  The softmax between them is the other wave's time on the SIMD: 32 exponentials, 16 of each of
@@ -991,6 +992,8 @@ static void launch_all(const PagedQuery& q, const PagedWork& w, const BatchView&
         // waves per SIMD: what the registers, and with 32 rows the LDS, leave room for; two for bf16 of d = 128, where a third
         // keeps the memory streams in shorter runs
         constexpr int FEW = E4M3 || D == 64 ? 4 : 2;
+        // one form for the whole launch, by its widest sequence: single tokens beside a draft of more than eight rows take the 32-row form,
+        // too (64 on 256 to 4096 positions of 8 kv heads, four query heads each, with one draft of 8 rows 99.4 us, of 16 rows 102.3)
         const unsigned grid = (unsigned)narrow_grid(w, bv, kv.Hkv);
         auto kern = w.narrow_rows <= 8 ? paged_narrow_kernel<D, E4M3, 8, FEW> : paged_narrow_kernel<D, E4M3, kNarrowRows, 3>;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, q, w, bv, kv, ws);
