@@ -222,3 +222,28 @@ def test_weights_of_short_sequences_keep_their_bits(torch, e4m3, d, heads, seqs)
     rms, stated, bf16 = (np.sqrt(np.mean(np.concatenate(x) ** 2)) for x in (err, as_stated, as_bf16))
     assert stated * 1.1 < bf16                               # the test can tell
     assert rms <= (stated + bf16) / 2, (rms, stated, bf16)
+
+
+def test_changes_on_the_stream_that_ran_the_batch_and_on_another(torch):
+    """Operations and a rebuild on one stream, a rebuild on another, results in between, and the end: no event of the first stream's
+    operations was ever recorded."""
+    import paper_2412_17246_amd as lib
+    L = lib.load_library()
+    w = World(torch, [(1, 100)], 4, 2, 64, 32, seed=89)
+    w.write_new()
+    want = w.attend()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    bytes_ = int(L.bz_batch_storage_bytes(1, 1, 256))
+    storage = (torch.empty(bytes_, dtype=torch.uint8, device="cuda"), torch.empty(2 * bytes_, dtype=torch.uint8, pin_memory=True), a)
+    outs, space = [torch.zeros_like(want) for _ in range(3)], w.workspace()
+    torch.cuda.synchronize()
+    w.batch = batch = lib.Batch(L, [0, 1], [0], [100], storage=storage)
+    w.attend(out=outs[0], workspace=space, stream=a)
+    batch.rebuild([0, 1], [0], [100], stream=a)
+    batch.rebuild([0, 1], [0], [100], stream=b)
+    w.attend(out=outs[1], workspace=space, stream=b)
+    batch.rebuild([0, 1], [0], [100], stream=b)
+    w.attend(out=outs[2], workspace=space, stream=b)
+    batch.close()                                            # waits
+    for out in outs:
+        assert torch.equal(out, want)
