@@ -860,6 +860,11 @@ int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
     for (bz_batch::Use& u : b->runs) {
         if (u.st == st) continue;
         const bool same_graph = u.capture && u.capture == capture;
+        // what a stream of this graph ran before it joined lies outside the graph, too
+        bool before_graph = false;
+        if (capture && !u.capture)
+            for (const bz_batch::Use& x : b->runs) before_graph |= x.st == u.st && x.capture == capture;
+        if (before_graph) continue;
         if (!same_graph && (rc = mark_use(u)) != BZ_OK) return rc;
         if (u.capture && !same_graph) continue;              // replays are the caller's to order
         HIP_TRY(hipStreamWaitEvent(st, u.ev, 0));

@@ -309,3 +309,38 @@ def test_grids_that_a_launch_cannot_have_are_refused(standin, fp32):
         assert L.bz_op_paged_read(C.byref(far), 0, 0, 1 << 20, 4096, 4096, S) == 0
 
     run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_a_graph_of_a_batch_that_ran_before(standin, fp32):
+    """The same behind eager runs on both streams: what is outside the graph is the caller's to order."""
+    def scenario():
+        import workloads as W
+        s = W.CONFIGS["tiny"]
+        pair = []
+        for st in (S, T):
+            cfg = B.make_config(s, max_seqs=1, max_seq_len=64, max_tokens=1, kv_tokens=64)
+            cfg.compute_stream, cfg.copy_stream = st, A
+            inst, sizes = C.c_void_p(), B.bz_sizes()
+            assert L.bz_create(C.byref(cfg), C.byref(inst)) == 0 and L.bz_query_sizes(C.byref(cfg), C.byref(sizes)) == 0
+            blob = C.create_string_buffer(sizes.layer_bytes)
+            for l in range(s.L):
+                assert L.bz_load_layer(inst, l, blob, sizes.layer_bytes) == 0
+            assert L.bz_kv_reserve(inst, 0, 64) == 0 and L.bz_frontier(inst) == s.L
+            pair.append(inst)
+        b, hidden = B.Batch(L, [0, 1], [0], [5]), C.create_string_buffer(4 * s.H)
+        for inst in pair:
+            assert L.bz_run_layers(inst, 0, 1, b.handle, hidden, 0) == 0
+        hip.standin_capture(S, 7)
+        for step in range(3):
+            assert L.bz_run_layers(pair[0], 0, 1, b.handle, hidden, 0) == 0
+            assert L.bz_signal_stream(pair[0], T) == 0           # the hidden states
+            hip.standin_work(S)
+            assert L.bz_run_layers(pair[1], 1, 2, b.handle, hidden, 0) == 0
+            assert hip.standin_unordered(S, T) > 0
+            assert L.bz_batch_advance(pair[0], b.handle) == 0
+            assert hip.standin_unordered(S, T) == 0
+        assert hip.standin_forbidden() == 0
+        hip.standin_capture(S, 0); hip.standin_capture(T, 0)
+
+    run(standin, scenario, fp32)
