@@ -66,10 +66,8 @@ struct bz_batch {
     // single operations, whose stream exists until the next change.)
     struct Use { hipStream_t st; hipEvent_t ev; bool unmarked, single; unsigned long long capture; };
     mutable std::vector<Use> runs;
-    hipStream_t changed_on = nullptr;
-    hipEvent_t changed_ev = nullptr;
-    bool changed_valid = false;
-    unsigned long long changed_capture = 0;
+    struct Change { hipStream_t on = nullptr; hipEvent_t ev = nullptr; bool valid = false; unsigned long long capture = 0; };
+    Change changed, changed_in_graph;       // the last eager one, and the last one if that was captured
 };
 
 namespace bz {

@@ -872,17 +872,37 @@ int wait_for_runs_elsewhere(bz_batch* b, hipStream_t st) {
     return BZ_OK;
 }
 
+// Orders stream `st` behind the batch's last change.
+int wait_for_change(const bz_batch* b, hipStream_t st) {
+    for (const bz_batch::Change* c : {&b->changed, &b->changed_in_graph}) {
+        if (!c->valid || c->on == st) continue;
+        // a change inside the graph that `st` is captured into follows the eager one already, or was refused
+        if (c == &b->changed && b->changed_in_graph.valid) {
+            unsigned long long capture = 0;
+            const int rc = capture_of(st, &capture);
+            if (rc) return rc;
+            if (capture && capture == b->changed_in_graph.capture) continue;
+        }
+        HIP_TRY(hipStreamWaitEvent(st, c->ev, 0));
+    }
+    return BZ_OK;
+}
+
 int mark_changed(bz_batch* b, hipStream_t st) {
-    if (!b->changed_ev) HIP_TRY(hipEventCreateWithFlags(&b->changed_ev, hipEventDisableTiming));
-    const int rc = capture_of(st, &b->changed_capture);
+    unsigned long long capture = 0;
+    const int rc = capture_of(st, &capture);
     if (rc) return rc;
-    HIP_TRY(hipEventRecord(b->changed_ev, st));
-    b->changed_on = st;
-    b->changed_valid = true;
+    bz_batch::Change& c = capture ? b->changed_in_graph : b->changed;
+    if (!c.ev) HIP_TRY(hipEventCreateWithFlags(&c.ev, hipEventDisableTiming));
+    HIP_TRY(hipEventRecord(c.ev, st));
+    c.on = st;
+    c.valid = true;
+    c.capture = capture;
+    if (!capture) b->changed_in_graph.valid = false;
     // this event is behind the stream's own operations as well, and stands for them: the stream may go now.  A graph's event stands
     // for the graph's alone.
     for (bz_batch::Use& u : b->runs)
-        if (u.st == st && (u.capture != 0) == (b->changed_capture != 0)) u.unmarked = u.single = false;
+        if (u.st == st && (u.capture != 0) == (capture != 0)) u.unmarked = u.single = false;
     return BZ_OK;
 }
 
@@ -918,13 +938,13 @@ BatchView batch_view(const bz_batch* b) {
 
 // Orders stream `st` behind the batch's last change if that was enqueued on another stream.
 int batch_before_run(const bz_batch* b, hipStream_t st) {
-    if (!b->changed_valid || b->changed_on == st) return BZ_OK;
+    const bz_batch::Change& last = b->changed_in_graph.valid ? b->changed_in_graph : b->changed;
+    if (!last.valid || last.on == st) return BZ_OK;
     unsigned long long capture = 0;
     const int rc = capture_of(st, &capture);
     if (rc) return rc;
-    if (capture && capture != b->changed_capture) return BZ_ESTATE;      // the wait would be for work outside the graph
-    HIP_TRY(hipStreamWaitEvent(st, b->changed_ev, 0));
-    return BZ_OK;
+    if (capture && capture != last.capture) return BZ_ESTATE;            // the wait would be for work outside the graph
+    return wait_for_change(b, st);
 }
 
 // A batch that can change on the device later (advance, rebuild), possibly on another stream, gets a marker behind the
@@ -976,13 +996,14 @@ int bz_batch_destroy(bz_batch* b) {
     }
     for (const bz_batch::Use& u : b->runs)
         if (!u.capture) HIP_TRY(hipEventSynchronize(u.ev));
-    if (b->changed_valid && !b->changed_capture) HIP_TRY(hipEventSynchronize(b->changed_ev));
+    if (b->changed.valid) HIP_TRY(hipEventSynchronize(b->changed.ev));
     for (int h = 0; h < 2; ++h) {
         if (b->staged_valid[h]) (void)hipEventSynchronize(b->staged_ev[h]);
         if (b->staged_ev[h]) (void)hipEventDestroy(b->staged_ev[h]);
     }
     for (const bz_batch::Use& u : b->runs) (void)hipEventDestroy(u.ev);
-    if (b->changed_ev) (void)hipEventDestroy(b->changed_ev);
+    for (hipEvent_t ev : {b->changed.ev, b->changed_in_graph.ev})
+        if (ev) (void)hipEventDestroy(ev);
     if (b->own_dev && b->dev) (void)hipFree(b->dev);
     delete b;
     return BZ_OK;
@@ -1027,7 +1048,8 @@ static int build_in_place(bz_batch* b, const bz_batch_desc* d, hipStream_t st) {
     // ... and runs enqueued on other streams must have read the device arrays before the new ones land
     int rc = wait_for_runs_elsewhere(b, st);
     if (rc) return rc;
-    if (b->changed_valid && b->changed_on != st) HIP_TRY(hipStreamWaitEvent(st, b->changed_ev, 0));
+    rc = wait_for_change(b, st);
+    if (rc) return rc;
     std::vector<int32_t> image;
     rc = describe_batch(d, b, image, b->dev_bytes);
     if (rc) return rc;
@@ -1093,7 +1115,8 @@ int bz_batch_advance(bz_instance* I, bz_batch* b) {
     // runs of this batch enqueued on another instance's stream still read the lengths and the work list
     int rc = wait_for_runs_elsewhere(b, I->compute);
     if (rc) return rc;
-    if (b->changed_valid && b->changed_on != I->compute) HIP_TRY(hipStreamWaitEvent(I->compute, b->changed_ev, 0));
+    rc = wait_for_change(b, I->compute);
+    if (rc) return rc;
     launch_batch_advance(b->d_kv_before, b->B, b->d_decode, b->d_seq_slot, b->n_decode, b->d_work, b->work_capacity,
                          I->compute);
     HIP_TRY(hipGetLastError());

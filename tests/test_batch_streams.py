@@ -344,3 +344,26 @@ def test_a_graph_of_a_batch_that_ran_before(standin, fp32):
         hip.standin_capture(S, 0); hip.standin_capture(T, 0)
 
     run(standin, scenario, fp32)
+
+
+@BUILDS
+def test_the_end_of_a_batch_waits_for_changes_before_a_captured_one(standin, fp32):
+    """Eager operations and an eager advance on S, then one more that is captured: its event says nothing of what was eager."""
+    def scenario():
+        import workloads as W
+        cfg = B.make_config(W.CONFIGS["tiny"], max_seqs=1, max_seq_len=64, max_tokens=1, kv_tokens=64)
+        cfg.compute_stream, cfg.copy_stream = S, A
+        inst = C.c_void_p()
+        assert L.bz_create(C.byref(cfg), C.byref(inst)) == 0
+        b = B.Batch(L, [0, 1], [0], [5])
+        assert append(b, S) == 0 and L.bz_batch_advance(inst, b.handle) == 0
+        eager = hip.standin_pending(S)
+        hip.standin_capture(S, 7)
+        assert append(b, S) == 0 and L.bz_batch_advance(inst, b.handle) == 0
+        hip.standin_capture(S, 0)
+        both = hip.standin_pending(S)
+        assert eager > 0 and both > eager
+        b.close()
+        assert hip.standin_pending(S) == both - eager and hip.standin_forbidden() == 0
+
+    run(standin, scenario, fp32)
