@@ -512,7 +512,7 @@ int bz_op_paged_append(const bz_batch* batch, const bz_paged_kv* kv, const void*
  * `rope`: as above, queries are rotated as they are read; NULL: they are rotated already, or there is no rotation.
  * Softmax and sums are float.  Rounded (not in the fp32 debug build) are the operands of the products, and the sum that divides is that
  * of the rounded weights.  In single tokens and sequences whose new tokens times n_q_heads / n_kv_heads are at most 32, a rotated query
- * has 16 bits and a weight 15, over BZ_KV_E4M3 11 where those rows exceed eight.  In longer ones a rotated query has 16 bits and a weight
+ * has 16 bits and a weight 15, over BZ_KV_E4M3 11 if any of them exceeds eight.  In longer ones a rotated query has 16 bits and a weight
  * is bf16; over BZ_KV_E4M3 both are fp16 there: 11 bits, fewer for weights below 2^-20 of a query's largest and for elements of a
  * query below 2^-27 of its largest, and below 2^-30 and 2^-38 they may count as nothing.  (Lent memory with no room for a batch's
  * list of short sequences makes long ones of them.)
